@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -13,7 +14,7 @@ LIB = os.path.join(HERE, "libellm.so")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 CALLS_SOURCE = os.path.join(CSRC, "python_calls.cpp")
 SOURCES = ["pool_core.cpp", "ellm_api.cpp", "kernels.hip"]
-HEADERS = ["pool_core.hpp", "kernels.hpp", "divide.hpp", "map_queue.hpp", os.path.join(ROOT, "include", "ellm.h")]
+HEADERS = ["pool_core.hpp", "kernels.hpp", "device.hpp", "divide.hpp", "map_queue.hpp", os.path.join(ROOT, "include", "ellm.h")]
 
 # packed-fp32 instructions are switched off for all device code of this library
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -31,16 +32,24 @@ def build(force: bool = True, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall",
-           "-Wno-unused-result", *DEVICE_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB]
     import numpy
     calls = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
              "-I", numpy.get_include(), CALLS_SOURCE, "-o", CALLS]
-    for c in (cmd, calls):
+    # every source by a compiler of its own, all at once: most of the time goes into the two files of kernels
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        compiles = [[hipcc, "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
+                     *(DEVICE_FLAGS if s.endswith(".hip") else []), "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c",
+                     os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objects)] + [calls]
+        link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objects, "-o", LIB]
         if verbose:
-            print(" ".join(c))
-        subprocess.run(c, check=True)
+            print("\n".join(" ".join(c) for c in [*compiles, link]))
+        running = [(c, subprocess.Popen(c)) for c in compiles]
+        status = [(c, p.wait()) for c, p in running]      # (all of them, also where one has failed)
+        for c, rc in status:
+            if rc:
+                raise subprocess.CalledProcessError(rc, c)
+        subprocess.run(link, check=True)
     return LIB
 
 
