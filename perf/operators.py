@@ -230,7 +230,7 @@ def prepare(case, seed):
     elif kind == "append":
         before, room = (lens, lens + case["new"]) if case["new"] else (np.zeros_like(lens), lens)
     elif kind == "copy":
-        before, room = np.concatenate([lens, np.zeros(B * case["copies"], np.int64)]), np.tile(lens, 1 + case["copies"])
+        before, room = np.concatenate([lens, np.zeros(B * case["copies"], np.int64)]), np.concatenate([lens, np.repeat(lens, case["copies"])])
     elif kind == "compact" and case["entry"] == "accept":
         room = lens + case["new"]
     st = _State(case, seed, before, room)
