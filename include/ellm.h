@@ -68,9 +68,19 @@ extern "C" {
 #define ELLM_CHUNK_MAPPED 1  /* backs exactly one (tensor, slot)                  */
 #define ELLM_CHUNK_BUSY   2  /* holds live activations; KV side may not touch it  */
 
-#define ELLM_BF16 1          /* the only element type: bfloat16, 2 bytes          */
+/* How a pool's rows are held (ellm_pool_desc.dtype). Rows go in and come out as bfloat16 either way. */
+#define ELLM_BF16 1          /* bfloat16, 2 bytes */
+#define ELLM_MXFP4 2         /* 4 bits and an 8-bit scale for 32 dims: a quarter (0.266) of the bytes, for
+                                a relative rms error of 0.115 on normal values.
+                                A block is 32 consecutive dims of a row, a = max |x| over it. Its scale is the
+                                smallest power of two s with a <= 6 s (exponents -127 .. 125), held as exponent + 127
+                                in 8 bits; x / s is rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (ties to the even
+                                code, 6 at most), with the sign of x in the 4th bit. The block stands for
+                                code * s. A block that holds a NaN or an infinity is NaN as a whole (scale 255). */
 
 #define ELLM_MAP_ALLOW_INFLATE 1u  /* map may take FREE activation-owned chunks (Sec. 2.2.1)  */
+
+#define ELLM_COMPACT_UNMAP 1u      /* ellm_kv_compact gives the slots behind the last token back */
 
 #define ELLM_POOL_METADATA_ONLY 1u /* pool flag: no device behind the pool. Host state machine
                                       only: append advances lengths without launching, offload and
@@ -115,7 +125,9 @@ typedef int32_t ellm_tensor_id;       /* dense handle >= 0            */
 /*
  * Pool geometry.
  *   bpt  = bytes per token of one layer = 2 (K and V) * n_kv_heads * head_dim * 2 bytes
- *   T_c  = tokens per chunk             = floor(chunk_bytes / bpt)        (must be >= 1)
+ *          (ELLM_MXFP4: 2 * n_kv_heads * (head_dim / 2 + head_dim / 32))
+ *   T_c  = tokens per chunk             = floor(chunk_bytes / bpt)        (must be >= 1;
+ *          ELLM_MXFP4: 256 and more are rounded down to a multiple of 16)
  *   n_chunks     = floor(device_bytes / chunk_bytes)
  *   n_host_slots = floor(host_bytes   / chunk_bytes)                      (may be 0)
  *
@@ -124,6 +136,9 @@ typedef int32_t ellm_tensor_id;       /* dense handle >= 0            */
  *   ((h * 2 + p) * T_c + r) * head_dim * 2 + d * 2.
  * Bytes past 2 * n_kv_heads * T_c * head_dim * 2 are slack: never read by attention, but copied
  * by offload / fetch, which always move whole chunks.
+ * ELLM_MXFP4: the codes of (h, p, r) are the head_dim / 2 bytes from ((h * 2 + p) * T_c + r) * head_dim / 2 on, dim d in the
+ * lower (d even) or upper half of byte d / 2; behind the codes of all rows, from n_kv_heads * T_c * head_dim on, its scales
+ * are the head_dim / 32 bytes from ((h * 2 + p) * T_c + r) * head_dim / 32 on.
  */
 typedef struct ellm_pool_desc {
   void*    device_base;      /* device, caller-owned, 256-byte aligned; NULL with METADATA_ONLY and
@@ -137,7 +152,7 @@ typedef struct ellm_pool_desc {
   uint16_t n_q_heads;
   uint16_t n_kv_heads;       /* n_q_heads % n_kv_heads == 0; group size G = n_q / n_kv <= 64      */
   uint16_t head_dim;         /* 64 or 128                                                         */
-  uint16_t dtype;            /* ELLM_BF16                                                         */
+  uint16_t dtype;            /* ELLM_BF16 or ELLM_MXFP4                                           */
   uint32_t max_tensors;      /* tensor handles 0 .. max_tensors-1                                 */
   uint32_t max_slots_per_tensor;
   uint32_t flags;            /* 0, ELLM_POOL_METADATA_ONLY or ELLM_POOL_DRIVER_MAPPED             */
@@ -288,6 +303,7 @@ int ellm_pool_set_act_busy(ellm_pool* pool, const int32_t* chunk_ids, int32_t n,
  *   k_new, v_new (device): [sum(n_new)][n_kv_heads][head_dim] bf16, request b's tokens start at row
  *   sum(n_new[0..b)). Token i of request b is written at position len_b + i; afterwards
  *   len_b += n_new[b]. Enqueued on `stream` (a hipStream_t); returns without waiting.
+ *   An ELLM_MXFP4 pool quantises the rows as it writes them.
  * Checks: batch < 0 -> INVALID; per request in order: bad or repeated handle, n_new < 0 -> INVALID;
  * len + n_new > max_tokens -> RANGE; slots covering the new tokens in ascending order: empty ->
  * UNMAPPED, on host -> NOT_RESIDENT. NULL k_new / v_new with tokens to write -> INVALID.
@@ -296,6 +312,46 @@ int ellm_pool_set_act_busy(ellm_pool* pool, const int32_t* chunk_ids, int32_t n,
  * been appended completely, rows and lengths, and the refused group and those after it not at all. */
 int ellm_kv_append(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, const int32_t* n_new,
                    const void* k_new, const void* v_new, void* stream);
+
+/* Read tokens out of tensors as dense rows: what a prompt's own attention over a cached prefix takes, and what an
+ * ELLM_MXFP4 pool makes of the rows it is given (its values are bfloat16 values exactly).
+ *   ids (host): batch handles, the same one as often as wanted. first, n_tokens (host): tokens first[b] ..
+ *   first[b] + n_tokens[b] - 1 of ids[b]; first NULL = from 0 on, n_tokens NULL = all from first on.
+ *   k_out, v_out (device): [sum(n_tokens)][n_kv_heads][head_dim] bf16, request after request. Enqueued on `stream`; returns
+ *   without waiting.
+ * Checks: batch < 0 -> INVALID; per request in order: bad handle, negative position or count -> INVALID; tokens past the
+ * length -> RANGE; their slots ascending: empty -> UNMAPPED, on host -> NOT_RESIDENT. NULL k_out / v_out with tokens to read ->
+ * INVALID; more than 2^30 / n_kv_heads tokens -> RANGE. Works in one launch per 128 requests, like ellm_kv_append. */
+int ellm_kv_read(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, const int64_t* first, const int64_t* n_tokens,
+                 void* k_out, void* v_out, void* stream);
+
+/* Copy tokens to the ends of other tensors: into empty ones this forks requests (several samples of one prompt, beams, a
+ * prefix that others share). Every chunk keeps exactly one owner, so a fork has its tokens to itself.
+ *   src, dst (host): n pairs of handles; a source may be given as often as wanted, a destination once and not as a source.
+ *   first, n_tokens (host): which tokens of src[i], as in ellm_kv_read. They are written at positions len .. of dst[i], whose
+ *   slots have to be mapped as for an append; afterwards len of dst[i] has grown by n_tokens[i].
+ *   Pairs that copy the same tokens are best neighbours: what neighbours have in common is read once (up to 128 pairs
+ *   at a time). Enqueued on `stream`; returns without waiting.
+ * Checks: n < 0 -> INVALID; every dst in order: bad or repeated handle -> INVALID; per pair in order: src as in ellm_kv_read, also a
+ * destination -> INVALID, dst: len + n_tokens > max_tokens -> RANGE, slots of the new tokens ascending: empty -> UNMAPPED, on
+ * host -> NOT_RESIDENT. More than 2^30 / n_kv_heads tokens -> RANGE. Works in one launch per 128 pairs, like ellm_kv_append. */
+int ellm_kv_copy(ellm_pool* pool, const ellm_tensor_id* src, const ellm_tensor_id* dst, int32_t n, const int64_t* first,
+                 const int64_t* n_tokens, void* stream);
+
+/* Keep some of the tokens of tensors, in place: evicted tokens go, drafts that were not accepted go, a finished turn is cut off.
+ *   ids (host): batch distinct handles. first, n_keep (host): of ids[b] the tokens before first[b] stay where they are, and
+ *   of the others n_keep[b]; NULL = 0 for all. keep (device): [sum(n_keep)] int32, request after request: their positions, ascending
+ *   without repetition, in first[b] .. len - 1. They become tokens first[b] .. in that order, and len becomes first[b] + n_keep[b].
+ *   Without n_keep (or with zeros) lengths are cut to first[b], and nothing is launched.
+ *   flags: ELLM_COMPACT_UNMAP: slots that hold no token afterwards are emptied, as by ellm_tensor_unmap_chunks.
+ *   keep is read by the launch. Positions that break the rules above make the rows behind first[b] undefined, and touch nothing else.
+ *   Enqueued on `stream`; returns without waiting.
+ * Checks: unknown flag, batch < 0 -> INVALID; per request in order: bad or repeated handle, negative position or count -> INVALID;
+ * first > len, n_keep > len - first -> RANGE; with n_keep > 0 the slots of first .. len - 1 ascending: empty -> UNMAPPED, on host ->
+ * NOT_RESIDENT. NULL keep with tokens to keep -> INVALID; more than 2^30 / n_kv_heads of them -> RANGE. Works in one launch per 128
+ * requests; lengths and slots of a group change when its launch has been accepted, as in ellm_kv_append. */
+int ellm_kv_compact(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, const int64_t* first, const int32_t* keep,
+                    const int64_t* n_keep, uint32_t flags, void* stream);
 
 /* Batched decode attention: one query token per request over its whole cached context.
  *   q (device): [batch][n_q_heads][head_dim] bf16; out (device): same shape, bf16.
@@ -469,7 +525,7 @@ int ellm_pool_profile_collect(ellm_pool* pool, float* ms, int32_t cap, int32_t* 
  *     sink: device, 4 bytes.
  *   debug_kv_stream_read: reads exactly the K/V rows a decode over `ids` would read, with the same
  *     work partition and load shape, and discards them: the ceiling of the access pattern.
- *     Same checks as ellm_decode_attention. */
+ *     Same checks as ellm_decode_attention; INVALID for pools that are not ELLM_BF16. */
 int ellm_debug_copy(void* dst, const void* src, uint64_t bytes, void* stream);
 int ellm_debug_stream_read(const void* src, uint64_t bytes, void* sink, void* stream);
 int ellm_debug_kv_stream_read(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, void* sink, void* stream);

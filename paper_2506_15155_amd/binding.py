@@ -31,6 +31,8 @@ lib = C.CDLL(LIB_PATH)
 ELLM_OWNER_KV, ELLM_OWNER_ACT = 0, 1
 ELLM_CHUNK_FREE, ELLM_CHUNK_MAPPED, ELLM_CHUNK_BUSY = 0, 1, 2
 ELLM_BF16 = 1
+ELLM_MXFP4 = 2
+ELLM_COMPACT_UNMAP = 1
 ELLM_MAP_ALLOW_INFLATE = 1
 ELLM_POOL_METADATA_ONLY = 1
 ELLM_POOL_DRIVER_MAPPED = 2
@@ -59,6 +61,7 @@ class _Desc(C.Structure):
 
 
 _i32p = C.POINTER(C.c_int32)
+_i64p = C.POINTER(C.c_int64)
 _i32_one = C.c_int32 * 1        # taken where _i32p is declared, and cheaper to make in place than a pointer
 _vp = C.c_void_p
 _sigs = {
@@ -84,6 +87,9 @@ _sigs = {
     "ellm_pool_transfer": [_vp, _i32p, C.c_int32, C.c_int],
     "ellm_pool_set_act_busy": [_vp, _i32p, C.c_int32, C.c_int],
     "ellm_kv_append": [_vp, _i32p, C.c_int32, _i32p, _vp, _vp, _vp],
+    "ellm_kv_read": [_vp, _i32p, C.c_int32, _i64p, _i64p, _vp, _vp, _vp],
+    "ellm_kv_copy": [_vp, _i32p, _i32p, C.c_int32, _i64p, _i64p, _vp],
+    "ellm_kv_compact": [_vp, _i32p, C.c_int32, _i64p, _vp, _i64p, C.c_uint32, _vp],
     "ellm_decode_attention": [_vp, _i32p, C.c_int32, _vp, _vp, C.c_float, _vp],
     "ellm_decode_attention_noalloc": [_vp, _i32p, C.c_int32, _vp, _vp, C.c_float, _vp],
     "ellm_kv_append_decode": [_vp, _i32p, C.c_int32, _vp, _vp, _vp, _vp, C.c_float, _vp],
@@ -171,6 +177,16 @@ def _i32(a):
         return arr, _i32_one.from_address(arr.ctypes.data), arr.size
 
 
+def _i64(a, count, what):
+    """(array to keep alive as long as the argument is used, the argument for _i64p) of a host array of 64-bit integers that
+    the library reads `count` entries of."""
+    if a is None:
+        return None, None
+    arr = np.ascontiguousarray(a, dtype=np.int64)
+    _holds(arr, count, what)
+    return arr, arr.ctypes.data_as(_i64p)
+
+
 def _holds(array, count, what):
     """The library reads `count` entries: an array of fewer is refused here, where its size is known (None: none is given)."""
     if array is not None and array.size < count:
@@ -197,8 +213,8 @@ def _stream(stream) -> int | None:
 
 def ellm_pool_create(device_buf, host_buf, chunk_bytes, n_q_heads, n_kv_heads, head_dim, max_tensors,
                      max_slots_per_tensor, initial_owner=None, flags=0, device_bytes=None, host_bytes=None,
-                     check=True):
-    """device_buf / host_buf: torch uint8 tensors (device / pinned host), or None. Returns the pool
+                     check=True, dtype=ELLM_BF16):
+    """dtype: ELLM_BF16 or ELLM_MXFP4. device_buf / host_buf: torch uint8 tensors (device / pinned host), or None. Returns the pool
     handle (an int); with check=False returns (rc, handle)."""
     d = _Desc()
     d.device_base = _ptr(device_buf)
@@ -207,7 +223,7 @@ def ellm_pool_create(device_buf, host_buf, chunk_bytes, n_q_heads, n_kv_heads, h
     d.host_base = _ptr(host_buf)
     d.host_bytes = host_bytes if host_bytes is not None else (host_buf.numel() * host_buf.element_size()
                                                                if host_buf is not None else 0)
-    d.chunk_bytes, d.n_q_heads, d.n_kv_heads, d.head_dim, d.dtype = chunk_bytes, n_q_heads, n_kv_heads, head_dim, ELLM_BF16
+    d.chunk_bytes, d.n_q_heads, d.n_kv_heads, d.head_dim, d.dtype = chunk_bytes, n_q_heads, n_kv_heads, head_dim, dtype
     d.max_tensors, d.max_slots_per_tensor, d.flags, d.reserved = max_tensors, max_slots_per_tensor, flags, 0
     own = None
     if initial_owner is not None:
@@ -392,6 +408,35 @@ def ellm_kv_append_decode(pool, ids, k_new, v_new, q, out, scale=0.0, stream=Non
         keep, p, n = _i32(ids)
         rc = lib.ellm_kv_append_decode(pool, p, n, _ptr(k_new), _ptr(v_new), _ptr(q), _ptr(out), float(scale), _stream(stream))
     return rc if rc >= 0 else _ret(rc, check)
+
+
+def ellm_kv_read(pool, ids, k_out, v_out, first=None, n_tokens=None, stream=None, check=True):
+    keep, p, n = _i32(ids)
+    keep_f, pf = _i64(first, n, "first")
+    keep_n, pn = _i64(n_tokens, n, "n_tokens")
+    return _ret(lib.ellm_kv_read(pool, p, n, pf, pn, _ptr(k_out), _ptr(v_out), _stream(stream)), check)
+
+
+def ellm_kv_copy(pool, src, dst, first=None, n_tokens=None, stream=None, check=True):
+    keep, p, n = _i32(src)
+    keep_d, pd, _ = _i32(dst)
+    _holds(keep_d, n, "dst")
+    keep_f, pf = _i64(first, n, "first")
+    keep_n, pn = _i64(n_tokens, n, "n_tokens")
+    return _ret(lib.ellm_kv_copy(pool, p, pd, n, pf, pn, _stream(stream)), check)
+
+
+def ellm_kv_compact(pool, ids, first=None, keep=None, n_keep=None, flags=0, stream=None, check=True):
+    """keep: device tensor of int32 positions. Without n_keep the tensors are cut to first."""
+    keep_i, p, n = _i32(ids)
+    keep_f, pf = _i64(first, n, "first")
+    keep_n, pn = _i64(n_keep, n, "n_keep")
+    if hasattr(keep, "numel") and keep_n is not None:
+        if keep.element_size() != 4 or not keep.is_contiguous():
+            raise ValueError("keep: 32-bit positions next to each other are read")
+        if keep.numel() < int(keep_n[:n].sum()):
+            raise ValueError(f"keep: {keep.numel()} entries where {int(keep_n[:n].sum())} are read")
+    return _ret(lib.ellm_kv_compact(pool, p, n, pf, _ptr(keep), pn, int(flags), _stream(stream)), check)
 
 
 def ellm_chunk_deflate_to_host(pool, tid, first_slot, n_slots, check=True):

@@ -175,7 +175,13 @@ struct ellm_pool {
   std::vector<int32_t> n_eff;
   std::vector<ellm::Move> moves;
   std::vector<ellm::BatchArgs> launches;
-  std::vector<int32_t> units_tmp, by64_tmp;
+  std::vector<int32_t> units_tmp, by64_tmp, both_ids;
+  std::vector<int64_t> zero_positions;
+  const int64_t* zeros(int32_t n) {
+    if ((int32_t)zero_positions.size() < n) zero_positions.resize(n, 0);
+    return zero_positions.data();
+  }
+  int32_t groups_done = 0;             // requests whose launches in_groups got through
 };
 
 namespace {
@@ -967,7 +973,7 @@ void plan_launch(ellm_pool* p, const int32_t* ids, int32_t n_req, int32_t q_row0
     const int64_t full = len / Tc;
     return full * chunk_units + (len - full * Tc + UNIT - 1) / UNIT;
   };
-  bool tiles = ellm::tile_kernel(p->geom.head_dim, p->geom.group, Tc);
+  bool tiles = !p->geom.fp4 && ellm::tile_kernel(p->geom.head_dim, p->geom.group, Tc);
   const int64_t slots = wave_slots(p), cus = p->compute_units;
   int64_t blocks = 0, longest = 0;     // what workgroups of several waves would take, in a launch small enough for that
   int32_t counted = 0;                 // not all of them once it is clear that there are too many
@@ -1081,6 +1087,78 @@ bool pair_up(ellm_pool* p, int64_t cap) {
 // a debug hook can make the n-th launch from now fail as if the runtime had refused it
 bool launch_refused(ellm_pool* p) { return p->fail_launch_in > 0 && --p->fail_launch_in == 0; }
 
+// ---- calls over tokens: quantised append, reading, copying, compacting ----
+// the kernels number tokens, and rows of a call's dense side, in 32 bits
+int fits_one_call(ellm_pool* p, int64_t total, const ellm_tensor_id* ids, int32_t n, const char* call) {
+  bool fits = total <= 0x7fffffffll / (2 * p->geom.n_kv_heads);
+  for (int32_t i = 0; i < n && fits; i++) fits = p->core->tensor(ids[i])->len + total <= 0x7fffffffll;
+  return fits ? ELLM_OK : set_err(ELLM_ERR_RANGE, std::string(call) + ": too many tokens in one call");
+}
+
+// Requests b0 .. b0 + nb - 1 of p->n_eff tokens each, at the ends of their tensors (first NULL) or from first[b] on. Returns
+// the dense side's rows of the requests before them.
+int64_t token_args(ellm_pool* p, ellm::TokenArgs& a, const ellm_tensor_id* ids, int32_t b0, int32_t nb, const int64_t* first) {
+  int64_t row0 = 0;
+  for (int32_t i = 0; i < b0; i++) row0 += p->n_eff[i];
+  a.n_req = a.blocks = 0;
+  int32_t rows = 0;
+  for (int32_t i = b0; i < b0 + nb; i++) {
+    const int32_t n = p->n_eff[i], k = a.n_req;
+    if (n == 0) continue;
+    a.tensor[k] = ids[i];
+    a.pos0[k] = (int32_t)(first ? first[i] : p->core->tensor(ids[i])->len);
+    a.n[k] = n;
+    a.row0[k] = rows;
+    a.block0[k] = a.blocks;
+    a.blocks += ellm::token_blocks(a.pos0[k], n);
+    rows += n;
+    a.n_req++;
+  }
+  return row0;
+}
+
+// One launch for every MAX_LAUNCH_REQ requests: launch(b0, nb) enqueues that of a group (LAUNCH_NOTHING: there is nothing to do for it),
+// done(b0, nb) follows each that was accepted. Groups before a refused one are complete, those behind it untouched;
+// p->groups_done requests are in the complete ones. ids (and more_ids): the tensors whose chunks the launches touch.
+constexpr int LAUNCH_NOTHING = -1;
+template <class Launch, class Done>
+int in_groups(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, hipStream_t stream, const char* what, Launch launch, Done done,
+              const ellm_tensor_id* more_ids = nullptr) {
+  int err = ELLM_OK, rc = ELLM_OK;
+  p->groups_done = 0;
+  for (int32_t b0 = 0; b0 < batch; b0 += ellm::MAX_LAUNCH_REQ) {
+    const int32_t nb = std::min<int32_t>(ellm::MAX_LAUNCH_REQ, batch - b0);
+    bool work = false;
+    for (int32_t i = b0; i < b0 + nb; i++) work |= i < (int32_t)p->n_eff.size() && p->n_eff[i] > 0;
+    if (work && launch_refused(p)) {
+      err = set_err(ELLM_ERR_HIP, std::string(what) + ": refused (debug hook)");
+      break;
+    }
+    if (!p->metadata_only) {
+      const int e = launch(b0, nb);
+      if (e > 0) {
+        err = hip_err((hipError_t)e, what);
+        break;
+      }
+    }
+    done(b0, nb);
+    p->groups_done = b0 + nb;
+  }
+  if (!p->metadata_only && p->groups_done > 0) {
+    rc = leave_compute(p, stream, ids, p->groups_done);
+    if (!rc && more_ids) rc = leave_compute(p, stream, more_ids, p->groups_done);
+  }
+  return err ? err : rc;
+}
+
+// as core_changed, behind launches of which some may have been refused
+int core_changed_with(ellm_pool* p, int rc) {
+  const std::string text = g_last_error;
+  const int changed = core_changed(p, ELLM_OK);
+  if (rc) g_last_error = text;
+  return rc ? rc : changed;
+}
+
 }  // namespace
 
 // ------------------------------------------------------------------------------------------------
@@ -1095,12 +1173,13 @@ int ellm_pool_create(const ellm_pool_desc* d, ellm_pool** out) {
   if (d->flags & ~(ELLM_POOL_METADATA_ONLY | ELLM_POOL_DRIVER_MAPPED) || d->reserved || (meta && vmm))
     return set_err(ELLM_ERR_INVALID, "pool_create: unknown flags");
   if (vmm && d->device_base) return set_err(ELLM_ERR_INVALID, "pool_create: a driver-mapped pool creates its own chunks; device_base must be NULL");
-  if (d->dtype != ELLM_BF16) return set_err(ELLM_ERR_INVALID, "pool_create: dtype must be ELLM_BF16");
+  if (d->dtype != ELLM_BF16 && d->dtype != ELLM_MXFP4) return set_err(ELLM_ERR_INVALID, "pool_create: dtype must be ELLM_BF16 or ELLM_MXFP4");
+  const bool fp4 = d->dtype == ELLM_MXFP4;
   if (d->head_dim != 64 && d->head_dim != 128) return set_err(ELLM_ERR_INVALID, "pool_create: head_dim must be 64 or 128");
   if (!d->n_kv_heads || !d->n_q_heads || d->n_q_heads % d->n_kv_heads || d->n_q_heads / d->n_kv_heads > 64)
     return set_err(ELLM_ERR_INVALID, "pool_create: n_q_heads must be a multiple (<= 64x) of n_kv_heads");
   if (!d->chunk_bytes || d->chunk_bytes % 256) return set_err(ELLM_ERR_INVALID, "pool_create: chunk_bytes must be a positive multiple of 256");
-  const uint64_t bpt = 2ull * d->n_kv_heads * d->head_dim * 2ull;
+  const uint64_t bpt = 2ull * d->n_kv_heads * (fp4 ? d->head_dim / 2ull + d->head_dim / ellm::FP4_BLOCK : d->head_dim * 2ull);
   if (d->chunk_bytes < bpt) return set_err(ELLM_ERR_INVALID, "pool_create: a chunk must hold at least one token");
   const uint64_t n_chunks = d->device_bytes / d->chunk_bytes;
   const uint64_t n_host = d->host_bytes / d->chunk_bytes;
@@ -1122,6 +1201,9 @@ int ellm_pool_create(const ellm_pool_desc* d, ellm_pool** out) {
   p->geom.chunk_bytes = d->chunk_bytes;
   p->geom.bytes_per_token = bpt;
   p->geom.tokens_per_chunk = (int32_t)(d->chunk_bytes / bpt);
+  p->geom.fp4 = fp4;
+  // large chunks of 4-bit rows hold whole units: the rows and scales of every (kv head, plane) then begin at a line
+  if (fp4 && p->geom.tokens_per_chunk >= ellm::FP4_WHOLE_UNITS) p->geom.tokens_per_chunk -= p->geom.tokens_per_chunk % ellm::UNIT_TOKENS;
   p->geom.n_q_heads = d->n_q_heads;
   p->geom.n_kv_heads = d->n_kv_heads;
   p->geom.head_dim = d->head_dim;
@@ -1219,6 +1301,15 @@ int ellm_kv_append(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, const
   int32_t most_new = 0;
   for (int32_t b = 0; b < batch; b++) most_new = std::max(most_new, n_new ? n_new[b] : 1);
   if (!p->metadata_only && (rc = enter_compute(p, stream, ids, batch, most_new))) return rc;
+  if (p->geom.fp4) {
+    return in_groups(p, ids, batch, stream, "kv_append launch", [&](int32_t b0, int32_t nb) {
+      ellm::TokenArgs a;
+      const int64_t row0 = token_args(p, a, ids, b0, nb, nullptr);
+      const size_t at = (size_t)row0 * p->geom.n_kv_heads * p->geom.head_dim * 2;
+      if (!a.blocks) return LAUNCH_NOTHING;
+      return ellm::launch_fp4_append(view_of(p), (const char*)k_new + at, (const char*)v_new + at, a, stream);
+    }, [&](int32_t b0, int32_t nb) { p->core->append_commit(ids + b0, nb, p->n_eff.data() + b0); });
+  }
   // One launch per group of MAX_LAUNCH_REQ requests; a group's lengths advance as soon as its launch
   // has been accepted, so rows written and lengths agree at every point, also when the runtime
   // refuses a later launch.
@@ -1251,6 +1342,119 @@ int ellm_kv_append(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, const
   }
   if (!p->metadata_only && done > 0 && (rc = leave_compute(p, stream, ids, done))) return rc;
   return err;
+}
+
+int ellm_kv_read(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, const int64_t* first, const int64_t* n_tokens, void* k_out,
+                 void* v_out, void* stream_) {
+  if (!p) return set_err(ELLM_ERR_INVALID, "NULL pool");
+  int64_t total = 0;
+  int rc = core_err(p, p->core->read_check(ids, batch, first, n_tokens, p->n_eff, &total));
+  if (rc) return rc;
+  if (total > 0 && (!k_out || !v_out)) return set_err(ELLM_ERR_INVALID, "kv_read: NULL k_out / v_out");
+  if ((rc = fits_one_call(p, total, ids, batch, "kv_read"))) return rc;
+  if (total == 0) return ELLM_OK;
+  if (p->metadata_only) return set_err(ELLM_ERR_NO_DEVICE, "kv_read: pool has no device");
+  hipStream_t stream = (hipStream_t)stream_;
+  if ((rc = enter_compute(p, stream, ids, batch, 0))) return rc;
+  return in_groups(p, ids, batch, stream, "kv_read launch", [&](int32_t b0, int32_t nb) {
+    ellm::TokenArgs a;
+    const int64_t row0 = token_args(p, a, ids, b0, nb, first ? first : p->zeros(batch));
+    const size_t at = (size_t)row0 * p->geom.n_kv_heads * p->geom.head_dim * 2;
+    if (!a.blocks) return LAUNCH_NOTHING;
+    return ellm::launch_read_tokens(view_of(p), p->geom.fp4, (char*)k_out + at, (char*)v_out + at, a, stream);
+  }, [](int32_t, int32_t) {});
+}
+
+int ellm_kv_copy(ellm_pool* p, const ellm_tensor_id* src, const ellm_tensor_id* dst, int32_t n, const int64_t* first,
+                 const int64_t* n_tokens, void* stream_) {
+  if (!p) return set_err(ELLM_ERR_INVALID, "NULL pool");
+  int64_t total = 0;
+  int rc = core_err(p, p->core->copy_check(src, dst, n, first, n_tokens, p->n_eff, &total));
+  if (rc) return rc;
+  if ((rc = fits_one_call(p, total, src, n, "kv_copy")) || (rc = fits_one_call(p, total, dst, n, "kv_copy"))) return rc;
+  if (total == 0) return ELLM_OK;
+  hipStream_t stream = (hipStream_t)stream_;
+  // both sides are work of this call
+  std::vector<int32_t>& both = p->both_ids;
+  both.assign(src, src + n);
+  both.insert(both.end(), dst, dst + n);
+  const int32_t most = *std::max_element(p->n_eff.begin(), p->n_eff.begin() + n);
+  if (!p->metadata_only && (rc = enter_compute(p, stream, both.data(), 2 * n, most))) return rc;
+  const int32_t per_block = ellm::copy_tokens_per_block(p->geom.head_dim, p->geom.fp4);
+  return in_groups(p, both.data(), n, stream, "kv_copy launch", [&](int32_t b0, int32_t nb) {
+    ellm::CopyTokenArgs a;
+    a.n_groups = a.blocks = 0;
+    int32_t d = 0;
+    for (int32_t i = b0; i < b0 + nb; i++) {
+      if (p->n_eff[i] == 0) continue;
+      const int32_t f = first ? (int32_t)first[i] : 0;
+      const int32_t g = a.n_groups - 1;
+      if (g < 0 || a.src[g] != src[i] || a.first[g] != f || a.n[g] != p->n_eff[i]) {
+        a.src[a.n_groups] = src[i];
+        a.first[a.n_groups] = f;
+        a.n[a.n_groups] = p->n_eff[i];
+        a.block0[a.n_groups] = a.blocks;
+        a.dst0[a.n_groups++] = d;
+        a.blocks += (p->n_eff[i] + per_block - 1) / per_block;
+      }
+      a.dst[d] = dst[i];
+      a.pos[d++] = (int32_t)p->core->tensor(dst[i])->len;
+    }
+    a.dst0[a.n_groups] = d;
+    if (!a.blocks) return LAUNCH_NOTHING;
+    return ellm::launch_copy_tokens(view_of(p), p->geom.fp4, a, stream);
+  }, [&](int32_t b0, int32_t nb) { p->core->append_commit(dst + b0, nb, p->n_eff.data() + b0); }, both.data() + n);
+}
+
+int ellm_kv_compact(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, const int64_t* first, const int32_t* keep,
+                    const int64_t* n_keep, uint32_t flags, void* stream_) {
+  if (!p) return set_err(ELLM_ERR_INVALID, "NULL pool");
+  if (flags & ~ELLM_COMPACT_UNMAP) return set_err(ELLM_ERR_INVALID, "kv_compact: unknown flags");
+  int64_t total = 0;
+  int rc = core_err(p, p->core->compact_check(ids, batch, first, n_keep, &total));
+  if (rc) return rc;
+  if (total > 0 && !keep) return set_err(ELLM_ERR_INVALID, "kv_compact: NULL keep");
+  if ((rc = fits_one_call(p, total, ids, batch, "kv_compact"))) return rc;
+  hipStream_t stream = (hipStream_t)stream_;
+  const bool unmap = (flags & ELLM_COMPACT_UNMAP) != 0;
+  p->n_eff.assign(batch, 0);
+  for (int32_t i = 0; i < batch && n_keep; i++) p->n_eff[i] = (int32_t)n_keep[i];
+  if (total == 0 || p->metadata_only) {
+    // only lengths change: nothing to launch and nothing to wait for
+    int err = ELLM_OK;
+    for (int32_t b0 = 0; b0 < batch && !err; b0 += ellm::MAX_LAUNCH_REQ) {
+      const int32_t nb = std::min<int32_t>(ellm::MAX_LAUNCH_REQ, batch - b0);
+      bool moves = false;
+      for (int32_t i = b0; i < b0 + nb; i++) moves |= p->n_eff[i] > 0;
+      if (moves && launch_refused(p)) err = set_err(ELLM_ERR_HIP, "kv_compact launch: refused (debug hook)");
+      else p->core->compact_commit(ids + b0, nb, first ? first + b0 : nullptr, n_keep ? n_keep + b0 : nullptr, unmap);
+    }
+    return unmap ? core_changed_with(p, err) : err;
+  }
+  if ((rc = enter_compute(p, stream, ids, batch, 0))) return rc;
+  int64_t key0 = 0;
+  rc = in_groups(p, ids, batch, stream, "kv_compact launch", [&](int32_t b0, int32_t nb) {
+    ellm::CompactArgs a;
+    a.n_req = 0;
+    int64_t in_group = 0;
+    for (int32_t i = b0; i < b0 + nb; i++) {
+      if (n_keep[i] == 0) continue;
+      a.tensor[a.n_req] = ids[i];
+      a.first[a.n_req] = first ? (int32_t)first[i] : 0;
+      a.n[a.n_req] = (int32_t)n_keep[i];
+      a.key0[a.n_req] = (int32_t)in_group;
+      a.len[a.n_req++] = (int32_t)p->core->tensor(ids[i])->len;
+      in_group += n_keep[i];
+    }
+    const int32_t* list = keep + key0;
+    key0 += in_group;
+    if (!a.n_req) return LAUNCH_NOTHING;
+    return ellm::launch_compact(view_of(p), p->geom.fp4, list, a, stream);
+  }, [&](int32_t, int32_t) {});
+  // the lengths and slots of the groups that were launched, behind the note of which chunks they touch
+  const int32_t done = p->groups_done;
+  p->core->compact_commit(ids, done, first, n_keep, unmap);
+  return unmap ? core_changed_with(p, rc) : rc;
 }
 
 int ellm_tensor_release(ellm_pool* p, ellm_tensor_id id) {
@@ -1341,6 +1545,7 @@ const char* ellm_debug_decode_kernel(ellm_pool* p, const ellm_tensor_id* ids, in
   if (core_err(p, p->core->decode_check(ids, batch, extra_tokens))) return nullptr;
   ellm::BatchArgs a;
   plan_launch(p, ids, std::min<int32_t>(batch, ellm::MAX_LAUNCH_REQ), 0, a, extra_tokens);
+  if (p->geom.fp4) return a.step_units > ellm::STEP_UNITS ? "decode_fp4_block_kernel" : "decode_fp4_kernel";
   if (a.unit_tokens == TILE_TOKENS) return "decode_tile_kernel";
   return a.step_units > ellm::STEP_UNITS ? "decode_block_kernel" : "decode_unit_kernel";
 }
@@ -1400,8 +1605,10 @@ static int decode_impl(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, c
     }
     if (launch_refused(p)) { err = set_err(ELLM_ERR_HIP, "decode partial launch: refused (debug hook)"); break; }
     const hipEvent_t ev_start = prof ? p->prof_ev[2 * p->prof_used] : nullptr, ev_stop = prof ? p->prof_ev[2 * p->prof_used + 1] : nullptr;
-    int e = pair ? ellm::launch_decode_pair(pv, q, k_new, v_new, ws, out, scale_log2, p->pair, stream, ev_start, ev_stop)
-                 : ellm::launch_decode_partial(pv, q, k_new, v_new, ws, out, scale_log2, launches[i], stream, ev_start, ev_stop);
+    const auto launch_one = p->geom.fp4 ? ellm::launch_fp4_decode : ellm::launch_decode_partial;
+    const auto launch_two = p->geom.fp4 ? ellm::launch_fp4_decode_pair : ellm::launch_decode_pair;
+    int e = pair ? launch_two(pv, q, k_new, v_new, ws, out, scale_log2, p->pair, stream, ev_start, ev_stop)
+                 : launch_one(pv, q, k_new, v_new, ws, out, scale_log2, launches[i], stream, ev_start, ev_stop);
     if (e) { err = hip_err((hipError_t)e, "decode partial launch"); break; }
     *n_launched += pair ? batch : launches[i].n_req;
     if (prof) p->prof_used++;
@@ -1692,7 +1899,7 @@ int ellm_debug_stream_read(const void* src, uint64_t bytes, void* sink, void* st
 }
 
 int ellm_debug_kv_stream_read(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, void* sink, void* stream_) {
-  if (!p || !sink) return set_err(ELLM_ERR_INVALID, "debug_kv_stream_read: bad argument");
+  if (!p || !sink || p->geom.fp4) return set_err(ELLM_ERR_INVALID, "debug_kv_stream_read: bad argument, or not a pool of bf16 rows");
   int rc = core_err(p, p->core->decode_check(ids, batch));
   if (rc) return rc;
   if (batch == 0) return ELLM_OK;

@@ -18,6 +18,8 @@ constexpr int STEP_UNITS = 4;         // units of a request that are worth a wav
 constexpr int BLOCK_UNITS = 16;       // small launches: units of a request that one workgroup of several waves takes
 constexpr int WIDE_UNITS = 32;        // launches up to twice as large: the most units that a workgroup takes,
 constexpr int WIDE_WAVES = 8;         // and its waves
+constexpr int FP4_BLOCK = 32;         // dims of a 4-bit row that have a scale in common
+constexpr int FP4_WHOLE_UNITS = 256;  // chunks of 4-bit rows that would hold at least so many tokens hold whole units
 constexpr int HEADS_PER_PASS = 16;    // q heads of a group the kernel that walks units handles in one pass over K and V
 constexpr int SIMDS_PER_CU = 4;       // a decode launch runs one wave on each SIMD
 constexpr int SHARE_WAVES = SIMDS_PER_CU;   // waves of a workgroup that walk a share each
@@ -147,6 +149,45 @@ struct alignas(64) AppendArgs {
   int32_t tensor[MAX_LAUNCH_REQ];
   int32_t len_before[MAX_LAUNCH_REQ];
   int32_t tok0[MAX_LAUNCH_REQ];    // first new-token row of request b, relative to this launch
+};
+
+// Tokens of tensors that one launch quantises into the cache, or reads out of it: of request b, positions pos0[b] ..
+// pos0[b] + n[b] - 1, rows row0[b] .. of the dense side. A workgroup takes the tokens of one block of TOKEN_BLOCK positions of
+// a request (a line of scales of heads of 128 then has one writer), for one kv head.
+constexpr int TOKEN_BLOCK = 32;
+struct alignas(64) TokenArgs {
+  int32_t n_req, blocks;           // requests with tokens; blocks of all of them
+  int32_t tensor[MAX_LAUNCH_REQ];
+  int32_t pos0[MAX_LAUNCH_REQ];
+  int32_t n[MAX_LAUNCH_REQ];
+  int32_t row0[MAX_LAUNCH_REQ];
+  int32_t block0[MAX_LAUNCH_REQ];  // blocks of the requests before this one
+};
+inline int32_t token_blocks(int64_t pos0, int64_t n) { return n > 0 ? (int32_t)((pos0 + n - 1) / TOKEN_BLOCK - pos0 / TOKEN_BLOCK + 1) : 0; }
+
+// Tokens copied from tensors to the ends of others. Copies of the same tokens, neighbours in the call, are a group: its
+// rows are read once and written to all of its destinations. A workgroup takes COPY_BYTES of rows of one kv head.
+constexpr int COPY_BYTES = 16 << 10;
+struct alignas(64) CopyTokenArgs {
+  int32_t n_groups, blocks;
+  int32_t src[MAX_LAUNCH_REQ];     // per group: tensor,
+  int32_t first[MAX_LAUNCH_REQ];   // first token,
+  int32_t n[MAX_LAUNCH_REQ];       // tokens,
+  int32_t block0[MAX_LAUNCH_REQ];  // blocks of tokens of the groups before it,
+  int32_t dst0[MAX_LAUNCH_REQ + 1];// its destinations: dst0[g] .. dst0[g + 1] - 1
+  int32_t dst[MAX_LAUNCH_REQ];     // per destination: tensor,
+  int32_t pos[MAX_LAUNCH_REQ];     // and length before the copy
+};
+
+// Tokens that move together: of request b, the tokens at keep[key0[b] + i] become tokens first[b] + i, i < n[b]; keep (device
+// memory) ascends, so none moves up. len: tokens that are there.
+struct alignas(64) CompactArgs {
+  int32_t n_req;
+  int32_t tensor[MAX_LAUNCH_REQ];
+  int32_t first[MAX_LAUNCH_REQ];
+  int32_t n[MAX_LAUNCH_REQ];
+  int32_t key0[MAX_LAUNCH_REQ];
+  int32_t len[MAX_LAUNCH_REQ];
 };
 
 struct PatchArgs {
@@ -289,6 +330,21 @@ int launch_decode_partial(const PoolView& pv, const void* q, const void* k_new, 
 int launch_decode_pair(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
                        PairArgs& a, hipStream_t stream, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
 int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const BatchArgs& a, hipStream_t stream);
+
+// ---- rows in 4 bits (fp4.hpp) ----
+int launch_fp4_append(const PoolView& pv, const void* k_new, const void* v_new, const TokenArgs& a, hipStream_t stream);
+// as launch_decode_partial and launch_decode_pair; the combine pass is the same
+int launch_fp4_decode(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
+                      const BatchArgs& a, hipStream_t stream, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
+int launch_fp4_decode_pair(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
+                           PairArgs& a, hipStream_t stream, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
+
+// ---- tokens of a cache; fp4: its rows are in 4 bits ----
+int launch_read_tokens(const PoolView& pv, bool fp4, void* k_out, void* v_out, const TokenArgs& a, hipStream_t stream);
+// tokens of a workgroup's block
+int copy_tokens_per_block(int head_dim, bool fp4);
+int launch_copy_tokens(const PoolView& pv, bool fp4, const CopyTokenArgs& a, hipStream_t stream);
+int launch_compact(const PoolView& pv, bool fp4, const int32_t* keep, const CompactArgs& a, hipStream_t stream);
 
 // Device address and size of the library's fixed workspace on the current device (resolved once per
 // device, kept afterwards). Allocates nothing. Returns 0 or a hipError_t value.

@@ -1,0 +1,540 @@
+// HIP kernels for gfx950: decode attention over a cache whose rows are held in 4 bits (fp4.hpp).
+//
+// For every query head:  s_t = scale * <q, K_t>,  w = softmax(s),  out = sum_t w_t V_t, one pass over the cache with the running
+// maximum and sum. A token of a kv head is 136 bytes (heads of 64: 68), a quarter of bf16's, so the arithmetic per byte is
+// four times as much: at the rate of a streaming read, 48 cycles of a SIMD per token, whatever the number of heads.
+//
+// The cut of a launch, what becomes of requests that several waves share, and the combine pass are those of the other attention
+// kernels (device.hpp); the work is dealt out in units of 16 rows of a chunk. A tile is U units. Both products are
+// 16x16x32 matrix instructions with up to 16 q heads of a kv head as columns:
+//   scores  S^T = K Q^T. Lane (g, c) of a wave (g = lane / 16, c = lane % 16) loads a quarter of row c: dims g D/4 .. of it, whose
+//      codes the conversion instruction turns into bf16 values, exactly, eight dims (a word) to an operand. The contraction
+//      index of lane group g is its own quarter of the dims; Q is laid out alike. Register i of a unit's result is the score
+//      of token 4 g + i for head c.
+//   softmax  a lane owns head c and four tokens of every unit; the weights are where the second product wants them, as the
+//      sum of two bf16 values (the next one below, and the rest), so they lose nothing that the result would show.
+//   PV      O^T = V^T P^T, two units at a time: contraction index of lane group g = its four tokens of either unit. Lane l loads a
+//      quarter of row l / 4; as bf16 values with their scale on them the rows of two units go through LDS, which hands them
+//      out transposed (a read that gives a lane 4 rows of one dim).
+// Products in 4 and 8 bits with scales (16x16x128) would take the codes as they are, but do not add up in 32 bits: their results
+// were 8e-5 of the sum of the products' magnitudes off.
+// The K rows of the next tile are asked for when this one's scores are formed, its V rows when this one's have gone to LDS.
+#include "fp4.hpp"
+
+namespace ellm {
+
+enum : uint32_t { T_FIRST = 1, T_LAST = 2, T_FIN = 4 };   // a tile starts a request here, ends it, ends the share
+template <int U>
+struct Fp4Tile {                     // what is known of a tile before its loads are issued (uniform)
+  int32_t n, b, part;                // units, request, partial slot of the request in this wave (-1: finished here)
+  uint32_t flags;                    // T_*
+  int32_t tail;                      // rows of its last unit
+  int32_t nv[U];                     // rows of each unit (0: the tile has no such unit)
+  int32_t r[U];                      // first row of the unit in its chunk
+  uint32_t at[U];                    // its chunk (table entry, or slot of the tensor's own range)
+  const char* base;                  // start of the pool, or of the tensor's range
+};
+
+// V rows of two units on their way through LDS: 32 bytes between rows keep the transposing reads off each other's banks
+template <int D> constexpr int STAGE_ROW = 2 * D + 32;
+template <int D> constexpr int STAGE_BYTES = 2 * UNIT_TOKENS * STAGE_ROW<D>;
+
+typedef short __attribute__((ext_vector_type(4))) s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
+
+// NW == 0: a wave walks its share, SW of them are a workgroup (SW == 1: single_waves()). NW > 0: NW waves share a step of up to NW * U units
+// of one request, one tile each, and add up through LDS. HEADS: q heads that LDS has room for.
+template <int D, int U, int HEADS, bool APPEND, bool DIRECT, int NW, int SW, class Args>
+__device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new,
+                                                const char* __restrict__ v_new, float* __restrict__ ws, uint16_t* __restrict__ out,
+                                                float scale_log2, int32_t g_first, int32_t n_heads, const Args& a, int32_t workgroup) {
+  constexpr int W = D / 32, ROW = FP4_ROW<D>, SCALES = FP4_SCALES<D>;     // words of a lane's quarter of a row
+  constexpr int NB = D / 16, F = D / 4;                                   // 16-dim blocks of the result; pieces of its rows
+  static_assert(U % 2 == 0, "PV takes two units at a time");
+  const int lane = threadIdx.x & 63, c = lane & 15, g16 = lane >> 4, vr = lane >> 2, vp = lane & 3;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Records<Args> records(a, lane);
+  wanted(a.n_req, a.waves_per_head, a.units_each, a.units_extra, a.by_waves.mul, a.by_waves.shift, a.step_units, a.q_row0);
+  wanted(pv.chunk_bytes, pv.tokens_per_chunk, pv.units_per_chunk, DIRECT ? 0 : pv.max_slots, pv.n_q_heads, pv.n_kv_heads, pv.group, g_first);
+  wanted(DIRECT ? nullptr : pv.base, DIRECT ? nullptr : pv.table, pv.vbase, q, pv.by_chunk.mul, pv.by_chunk.shift, pv.by_units.mul, pv.by_units.shift);
+  const int32_t Tc = pv.tokens_per_chunk;
+  const uint32_t plane = (uint32_t)Tc * ROW, scale_plane = (uint32_t)Tc * SCALES;      // from K to V of the same head
+
+  const int32_t index = NW ? workgroup : workgroup * SW + wave;
+  const Share<Args> sh = locate_share(a, records, NW ? index : min(index, a.waves_per_head * pv.n_kv_heads - 1), lane);
+  const int32_t g = sh.g;
+  const int32_t hq0 = g * pv.group + g_first;        // first q head handled here
+  const int32_t head = min(c, n_heads - 1);          // lanes beyond the last head repeat it and write nothing
+  const uint64_t head_rows = (uint64_t)(2 * g) * plane, head_scales = fp4_scales_at<D>(pv) + (uint64_t)(2 * g) * scale_plane;
+
+  // ---- cursor: the next tile to be asked for ----
+  int32_t cb = sh.b, rem_share = sh.n_units, len, slot, r, rem_req, part;
+  uint32_t first = T_FIRST;
+  TensorWalk walk;
+  const typename Args::Req& first_rq = sh.first;
+  {
+    const typename Args::Req& rq = first_rq;
+    len = rq.len;
+    walk = tensor_walk<DIRECT>(pv, rq.tensor);
+    constexpr int32_t STEP_WAVES = NW ? NW : 1;
+    const int32_t mine = NW ? wave * a.step_units / STEP_WAVES : 0;     // (at most U apart from one wave to the next)
+    const int32_t u0 = (sh.u_lo - rq.unit_prefix) * a.step_units + mine;
+    rem_req = units_of(len, pv, pv.units_per_chunk) - u0;
+    if (NW) rem_share = min((wave + 1) * a.step_units / STEP_WAVES - mine, rem_req);
+    else if (a.step_units > 1) rem_share = min(rem_share * a.step_units, rem_req);
+    slot = divide(u0, pv.by_units);
+    r = (u0 - slot * pv.units_per_chunk) * UNIT_TOKENS;
+    part = rq.n_part == 1 ? -1 : rq.part0 + (sh.w - rq.wave_first);    // (which slot: only where a workgroup is a step)
+  }
+  auto advance = [&](Fp4Tile<U>& t) __attribute__((always_inline)) {
+    t.n = min(U, min(rem_share, rem_req));
+    t.b = cb;
+    t.part = part;
+    t.flags = first;
+    t.base = DIRECT ? walk.tbase : pv.base;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      if (u == 0 || u < t.n) {
+        t.at[u] = DIRECT ? (uint32_t)slot : (uint32_t)walk.trow[slot];
+        t.r[u] = r;
+        t.nv[u] = min(UNIT_TOKENS, min(Tc - r, len - (slot * Tc + r)));
+        t.tail = t.nv[u];
+        if (u < t.n - 1 || (t.n > 0 && rem_req > t.n)) {   // there is a next unit of this request
+          r += UNIT_TOKENS;
+          if (r >= Tc) { r = 0; slot += 1; }
+        }
+      } else {
+        t.at[u] = t.at[u - 1];
+        t.r[u] = t.r[u - 1];
+        t.nv[u] = 0;
+      }
+    }
+    if (t.n == 0) t.nv[0] = 0;                       // past the end of the share
+    rem_req -= t.n;
+    rem_share -= t.n;
+    first = 0;
+    if (rem_req == 0) {
+      t.flags |= T_LAST;
+      first = T_FIRST;
+    }
+    if (rem_share == 0) t.flags |= T_FIN;
+    if (rem_req == 0 && rem_share > 0) {
+      cb += 1;
+      const typename Args::Req rq = a.req[cb];
+      len = rq.len;
+      rem_req = units_of(len, pv, pv.units_per_chunk);
+      walk = tensor_walk<DIRECT>(pv, rq.tensor);
+      slot = 0;
+      r = 0;
+      part = rq.n_part == 1 ? -1 : rq.part0;
+    }
+  };
+  // a unit's K rows and scales (V's: plane, scale_plane further on)
+  auto rows_base = [&](const Fp4Tile<U>& t, int u) __attribute__((always_inline)) {
+    return const_cast<char*>(t.base) + (uint64_t)t.at[u] * pv.chunk_bytes + head_rows + (uint32_t)t.r[u] * ROW;
+  };
+  auto scales_base = [&](const Fp4Tile<U>& t, int u) __attribute__((always_inline)) {
+    return const_cast<char*>(t.base) + (uint64_t)t.at[u] * pv.chunk_bytes + head_scales + (uint32_t)t.r[u] * SCALES;
+  };
+  // how many of the rows are in the chunk: all but the one that a fused append is about to put there
+  auto there = [&](const Fp4Tile<U>& t, int u) __attribute__((always_inline)) {
+    return t.nv[u] - (APPEND && (t.flags & T_LAST) && u == t.n - 1 ? 1 : 0);
+  };
+
+  // ---- loads ----
+  // Buffer loads with the unit's rows as their range: rows past its end, and units that the tile does not have, come back as
+  // zeros (codes of 0, scales of 2^-127) without a memory access, and the number of loads does not depend on the tile.
+  struct Quarter { uint32_t w[W]; };                 // of a row of codes
+  Quarter k[U], v[U];
+  uint32_t ks[U], vs[U];
+  words4_t qr[W];
+  uint32_t kn[D / 8], vn[D / 8];                     // the new row's quarter, in bf16
+  const int scale_of_quarter = D == 128 ? 1 : 2;     // quarters that share a scale
+  auto load_quarter = [&](__amdgpu_buffer_rsrc_t rows, int32_t at) __attribute__((always_inline)) {
+    Quarter x;
+    if constexpr (W == 4) {
+      const words4_t w = __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, CPOL_NT);
+      x.w[0] = w.x; x.w[1] = w.y; x.w[2] = w.z; x.w[3] = w.w;
+    } else {
+      const words2_t w = __builtin_amdgcn_raw_buffer_load_b64(rows, at, 0, CPOL_NT);
+      x.w[0] = w.x; x.w[1] = w.y;
+    }
+    return x;
+  };
+  auto new_row = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+    return ((int64_t)(a.q_row0 + t.b) * pv.n_kv_heads + g) * (2 * D);
+  };
+  auto load_new = [&](const char* from, int32_t quarter, uint32_t (&x)[D / 8]) __attribute__((always_inline)) {
+    const gptr_t p = (gptr_t)from + quarter * (D / 2);
+#pragma unroll
+    for (int i = 0; i < D / 32; i++) {
+      const words4_t w = *(const __attribute__((address_space(1))) words4_t*)(p + 16 * i);
+      x[4 * i] = w.x; x[4 * i + 1] = w.y; x[4 * i + 2] = w.z; x[4 * i + 3] = w.w;
+    }
+  };
+  auto issue_k = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+    if (t.flags & T_FIRST) {
+      const gptr_t qp = (gptr_t)(q + ((int64_t)(a.q_row0 + t.b) * pv.n_q_heads + hq0 + head) * D) + g16 * (D / 2);
+#pragma unroll
+      for (int w = 0; w < W; w++) qr[w] = *(const __attribute__((address_space(1))) words4_t*)(qp + w * 16);
+    }
+    if (APPEND && (t.flags & T_LAST)) load_new(k_new + new_row(t), g16, kn);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int32_t rows = there(t, u);
+      k[u] = load_quarter(buffer_at(rows_base(t, u), rows * ROW), c * ROW + g16 * (4 * W));
+      ks[u] = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(scales_base(t, u), rows * SCALES), c * SCALES + g16 / scale_of_quarter, 0, CPOL_NT);
+    }
+  };
+  auto issue_v = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+    if (APPEND && (t.flags & T_LAST)) load_new(v_new + new_row(t), vp, vn);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int32_t rows = there(t, u);
+      v[u] = load_quarter(buffer_at(rows_base(t, u) + plane, rows * ROW), lane * (4 * W));
+      vs[u] = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(scales_base(t, u) + scale_plane, rows * SCALES), vr * SCALES + vp / scale_of_quarter, 0, CPOL_NT);
+    }
+  };
+  // A quarter of a new row in 4 bits; `partner`: the larger magnitude of this lane's and that of the lane that has the other half of a
+  // block (heads of 64)
+  auto quantise = [&](const uint32_t (&x)[D / 8], Quarter& codes, uint32_t& scale, auto partner) __attribute__((always_inline)) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < D / 8; i++) top = max_magnitudes(top, x[i]);
+    if constexpr (D == 64) top = partner(top);
+    scale = fp4_scale(top);
+#pragma unroll
+    for (int w = 0; w < W; w++) {
+      const uint32_t eight[4] = {x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
+      codes.w[w] = fp4_codes(eight, scale);
+    }
+  };
+  // stored where it belongs: row `row` of the unit whose rows and scales begin there, quarter `quarter`
+  auto store_new = [&](char* rows, char* scales, int32_t row, int32_t quarter, const Quarter& codes, uint32_t scale) __attribute__((always_inline)) {
+    const gwptr_t to = (gwptr_t)rows + row * ROW + quarter * (4 * W);
+    if constexpr (W == 4) *(__attribute__((address_space(1))) words4_t*)to = words4_t{codes.w[0], codes.w[1], codes.w[2], codes.w[3]};
+    else *(__attribute__((address_space(1))) words2_t*)to = words2_t{codes.w[0], codes.w[1]};
+    if (quarter % scale_of_quarter == 0) *(__attribute__((address_space(1))) uint8_t*)((gwptr_t)scales + row * SCALES + quarter / scale_of_quarter) = (uint8_t)scale;
+  };
+
+  // ---- arithmetic ----
+  float m = NEG_BIG, l = 0.f;
+  f32x4_t acc[NB], s[U];
+  auto scores = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+    if (APPEND && (t.flags & T_LAST)) {
+      // the new token's K row takes the place of what the loads found there, and goes into the chunk (a unit that the tile
+      // does not have has the address of the one before it)
+      Quarter codes;
+      uint32_t scale;
+      quantise(kn, codes, scale, [](uint32_t x) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return max_magnitudes(r[0], r[1]);
+      });
+      const int32_t rl = t.tail - 1;
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const bool mine = u == t.n - 1 && c == rl;
+#pragma unroll
+        for (int w = 0; w < W; w++) k[u].w[w] = mine ? codes.w[w] : k[u].w[w];
+        ks[u] = mine ? scale : ks[u];
+      }
+      if (c == rl) store_new(rows_base(t, U - 1), scales_base(t, U - 1), rl, g16, codes, scale);
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      f32x4_t d = {0.f, 0.f, 0.f, 0.f};
+      const float scale = fp4_scale_float(ks[u]);
+#pragma unroll
+      for (int w = 0; w < W; w++) d = mfma16(fp4_values(k[u].w[w], scale), qr[w], d);
+      s[u] = d * scale_log2;
+    }
+  };
+  auto weigh = [&](const Fp4Tile<U>& t, char* stage) __attribute__((always_inline)) {
+    if (t.flags & T_FIRST) {
+      m = NEG_BIG;
+      l = 0.f;
+#pragma unroll
+      for (int n = 0; n < NB; n++) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    bool full = true;
+#pragma unroll
+    for (int u = 0; u < U; u++) full &= t.nv[u] == UNIT_TOKENS;
+    if (!full) {
+      // scores of rows that are not there
+#pragma unroll
+      for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) s[u][i] = 4 * g16 + i < t.nv[u] ? s[u][i] : -INFINITY;
+    }
+    if (APPEND && (t.flags & T_LAST)) {
+      // the new token's V row
+      Quarter codes;
+      uint32_t scale;
+      quantise(vn, codes, scale, [](uint32_t x) { return max_magnitudes_xor1(x); });
+      const int32_t rl = t.tail - 1;
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const bool mine = u == t.n - 1 && vr == rl;
+#pragma unroll
+        for (int w = 0; w < W; w++) v[u].w[w] = mine ? codes.w[w] : v[u].w[w];
+        vs[u] = mine ? scale : vs[u];
+      }
+      if (vr == rl) store_new(rows_base(t, U - 1) + plane, scales_base(t, U - 1) + scale_plane, rl, vp, codes, scale);
+    }
+    float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+#pragma unroll
+    for (int u = 1; u < U; u++) mx = fmaxf(mx, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
+    const float mn = fmaxf(m, max_xor32(max_xor16(mx)));
+    if (__builtin_amdgcn_ballot_w64(mn > m)) {       // some head has a new maximum
+      const float alpha = fast_exp2(m - mn);
+      l *= alpha;
+#pragma unroll
+      for (int n = 0; n < NB; n++) acc[n] *= alpha;
+      m = mn;
+    }
+#pragma unroll
+    for (int u = 0; u < U; u += 2) {
+      uint32_t pb[4], pr[4];
+#pragma unroll
+      for (int h = 0; h < 4; h++) {
+        const f32x4_t& x = s[u + h / 2];
+        const float p0 = fast_exp2(x[2 * (h & 1)] - m), p1 = fast_exp2(x[2 * (h & 1) + 1] - m);
+        l += p0 + p1;
+        const uint32_t b0 = bf16_below(p0), b1 = bf16_below(p1);
+        pb[h] = __builtin_amdgcn_perm(b1, b0, 0x07060302);
+        pr[h] = pack_bf16(p0 - __uint_as_float(b0), p1 - __uint_as_float(b1));
+      }
+      // rows of units u and u + 1 to LDS: row 16 j + vr, dims of quarter vp
+#pragma unroll
+      for (int j = 0; j < 2; j++) {
+        const float scale = fp4_scale_float(vs[u + j]);
+#pragma unroll
+        for (int w = 0; w < W; w++)
+          *reinterpret_cast<words4_t*>(stage + (UNIT_TOKENS * j + vr) * STAGE_ROW<D> + vp * (D / 2) + w * 16) = fp4_values(v[u + j].w[w], scale);
+      }
+      const words4_t weights = {pb[0], pb[1], pb[2], pb[3]}, rest = {pr[0], pr[1], pr[2], pr[3]};
+      // a block of 16 dims: lane (g, c) addresses 4 dims of row 4 g + c / 4 and gets dim c of rows 4 g .. 4 g + 3
+      char* const from = stage + (4 * g16 + (c >> 2)) * STAGE_ROW<D> + (c & 3) * 8;
+#pragma unroll
+      for (int n = 0; n < NB; n++) {
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + 32 * n)),
+                      hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + UNIT_TOKENS * STAGE_ROW<D> + 32 * n));
+        const words2_t l2 = __builtin_bit_cast(words2_t, lo), h2 = __builtin_bit_cast(words2_t, hi);
+        const words4_t va = {l2.x, l2.y, h2.x, h2.y};
+        acc[n] = mfma16(va, rest, mfma16(va, weights, acc[n]));
+      }
+    }
+  };
+  // which piece of a row, in the order of partial_dim() for units, has dims 16 n + 4 g16 .. + 3
+  auto piece = [&](int n) __attribute__((always_inline)) {
+    if constexpr (D == 128) {
+      const int e = 2 * n + (g16 >> 1);
+      return (e & 3) * 8 + (g16 & 1) * 4 + (e >> 2);
+    } else {
+      return 4 * g16 + n;
+    }
+  };
+
+  if constexpr (NW > 0) {
+    constexpr int ROWF = D + 4;                        // a row of a head's accumulators, padded against bank conflicts
+    // a wave's V rows on their way through LDS, and then its sums
+    constexpr int MINE = std::max<int>(STAGE_BYTES<D>, HEADS * ROWF * 4);
+    __shared__ __attribute__((aligned(16))) char lds[NW][MINE];
+    __shared__ float2 ml[NW][HEADS];
+    float* const mine = reinterpret_cast<float*>(lds[wave]);
+    if (rem_share > 0) {
+      Fp4Tile<U> t;
+      advance(t);
+      issue_k(t);
+      issue_v(t);
+      __builtin_amdgcn_sched_barrier(0);
+      scores(t);
+      weigh(t, lds[wave]);
+      const float L = add_xor32(add_xor16(l));
+      if (c < n_heads) {
+#pragma unroll
+        for (int n = 0; n < NB; n++)
+          *reinterpret_cast<float4*>(mine + c * ROWF + piece(n) * 4) = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+        if (g16 == 0) ml[wave][c] = make_float2(m, L);
+      }
+    } else {
+      // nothing left for this wave: zeros, whose weight is 0
+      if (lane < n_heads) ml[wave][lane] = make_float2(-INFINITY, 0.f);
+      for (int i = lane; i < n_heads * F; i += 64) *reinterpret_cast<float4*>(mine + i / F * ROWF + i % F * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __syncthreads();
+    // every wave takes 64 columns (pieces of the heads' rows in order), which need no other wave from here on
+    const int32_t n_cols = n_heads * F;
+    static_assert(HEADS * F <= NW * 64, "a thread for every column");
+    const int32_t x = threadIdx.x, h = x / F, f = x % F;
+    if (wave * 64 >= n_cols) return;
+    Sum sum = {NEG_BIG, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    if (x < n_cols) {
+      float2 p[NW];
+      float4 v4[NW];
+#pragma unroll
+      for (int w = 0; w < NW; w++) {
+        p[w] = ml[w][h];
+        v4[w] = *reinterpret_cast<const float4*>(lds[w] + (h * ROWF + f * 4) * 4);
+      }
+#pragma unroll
+      for (int w = 0; w < NW; w++) sum.M = fmaxf(sum.M, p[w].x);
+#pragma unroll
+      for (int w = 0; w < NW; w++) add(sum, p[w].y, v4[w], fast_exp2(p[w].x - sum.M));
+      if (part < 0) write_out<D>(pv, out, a, cb, g, g_first, x, sum);
+      else leave_partial<D>(pv, ws, a, part, g, g_first, n_heads, x, sum);
+    }
+    // one of several blocks of its request: the last of them to get here adds their results up
+    const int32_t n_part = first_rq.n_part;
+    if (n_part == 1 || n_part > a.merge_parts) return;
+    stores_done();
+    uint32_t before = 0;
+    if (lane == 0) before = count_in(pv, g * a.waves_per_head + first_rq.wave_first + wave % n_part, wave, n_part);
+    const Partials<D> all(ws, a.ws_slots, (int64_t)g * a.parts_per_head + first_rq.part0, n_part, held(pv.group), g_first, n_heads);
+    if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)n_part - 1u) return;
+    Sum all_of[1];
+    all.template sum<1, 8, 16>(all_of, x, 0, 0, n_part);
+    if (x < n_cols) write_out<D>(pv, out, a, cb, g, g_first, x, all_of[0]);
+    return;
+  }
+  __shared__ __attribute__((aligned(16))) char stages[NW ? 1 : SW][NW ? 1 : STAGE_BYTES<D>];
+  __shared__ __attribute__((aligned(16))) Results<D, SW == 1 ? 1 : HEADS> results;     // (SW == 1: not used)
+  char* const stage = stages[NW ? 0 : wave];
+  auto finish = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+    const float L = add_xor32(add_xor16(l));
+    if (c >= n_heads) return;
+    if (t.part < 0) {
+      // the whole request lay inside this wave's share: normalise, round and write the output rows
+      const float inv = 1.f / L;
+      uint16_t* o = out + ((int64_t)(a.q_row0 + t.b) * pv.n_q_heads + hq0 + c) * D + 4 * g16;
+#pragma unroll
+      for (int n = 0; n < NB; n++)
+        *reinterpret_cast<uint2*>(o + 16 * n) = make_uint2(pack_bf16(acc[n][0] * inv, acc[n][1] * inv), pack_bf16(acc[n][2] * inv, acc[n][3] * inv));
+    } else if constexpr (SW == 1) {
+      // one of several waves of the request: a partial result
+      const int64_t row = ((int64_t)g * a.parts_per_head + t.part) * pv.group + g_first + c;
+#pragma unroll
+      for (int n = 0; n < NB; n++)
+        *reinterpret_cast<float4*>(ws + row * D + piece(n) * 4) = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+      if (g16 == 0) *reinterpret_cast<float2*>(ws + (int64_t)a.ws_slots * pv.group * D + row * WS_ML) = make_float2(m, L);
+    } else {
+      // its results meet the others' in LDS
+      const int32_t to = 2 * wave + (t.b == sh.b ? 0 : 1);
+#pragma unroll
+      for (int n = 0; n < NB; n++)
+        results.rows[to][c][piece(n)] = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+      if (g16 == 0) results.ml[to][c] = make_float2(m, L);
+      if (lane == 0) results.whose[to] = g * MAX_LAUNCH_REQ + t.b;
+    }
+  };
+  // No exit before the round's last load (the share's last round asks for rows it does not use): what is in flight when a
+  // tile is waited for is the same on every path, so the compiler counts the loads exactly.
+  if (index < a.waves_per_head * pv.n_kv_heads) {
+    Fp4Tile<U> t, next;
+    advance(t);
+    issue_k(t);
+    issue_v(t);
+    __builtin_amdgcn_sched_barrier(0);               // the loads stay where they are asked for
+    if constexpr (SW > 1) results.clear(wave, lane);
+    advance(next);
+    uint32_t done;
+    do {
+      scores(t);
+      issue_k(next);
+      __builtin_amdgcn_sched_barrier(0);
+      weigh(t, stage);
+      if (t.flags & (T_LAST | T_FIN)) finish(t);     // the request ends here, or the share does
+      done = t.flags & T_FIN;
+      issue_v(next);
+      __builtin_amdgcn_sched_barrier(0);
+      t = next;
+      advance(next);
+    } while (!done);
+  } else if constexpr (SW > 1) {
+    results.clear(wave, lane);
+  }
+  if constexpr (SW > 1) end_shares<D, HEADS>(pv, ws, out, a, records, results, g_first, n_heads, workgroup, wave, lane);
+}
+
+template <int D, int U, int HEADS, int SW, bool APPEND, bool DIRECT, class Args>
+__global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(2, 2))) void decode_fp4_kernel(
+    PoolView pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new, const char* __restrict__ v_new,
+    float* __restrict__ ws, uint16_t* __restrict__ out, float scale_log2, int32_t g_first, int32_t n_heads, Args a) {
+  in_launch(pv, ws, a, [&](const PoolView& pv, float* ws, const auto& a, int32_t workgroup) __attribute__((always_inline)) {
+    decode_fp4_body<D, U, HEADS, APPEND, DIRECT, 0, SW>(pv, q, k_new, v_new, ws, out, scale_log2, g_first, n_heads, a, workgroup);
+  });
+}
+template <int D, int U, int HEADS, int NW, bool APPEND, bool DIRECT, class Args>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void decode_fp4_block_kernel(
+    PoolView pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new, const char* __restrict__ v_new,
+    float* __restrict__ ws, uint16_t* __restrict__ out, float scale_log2, int32_t g_first, int32_t n_heads, Args a) {
+  in_launch(pv, ws, a, [&](const PoolView& pv, float* ws, const auto& a, int32_t workgroup) __attribute__((always_inline)) {
+    decode_fp4_body<D, U, HEADS, APPEND, DIRECT, NW, 1>(pv, q, k_new, v_new, ws, out, scale_log2, g_first, n_heads, a, workgroup);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// launchers
+// ---------------------------------------------------------------------------------------------
+constexpr int FP4_UNITS = 4;         // units per tile
+
+// a: the plan, or one of the two in `args`, which run the same kernel; workgroups: of all of it
+template <int D, bool APPEND, bool DIRECT, class Args>
+static int launch_fp4_i(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
+                        const BatchArgs& a, const Args& args, unsigned workgroups, hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop) {
+  constexpr bool PAIR = std::is_same_v<Args, PairArgs>;
+  // a group of more than HEADS_PER_PASS q heads is covered by several launches over the same K/V: the first of them takes the
+  // start time, the last one the end time
+  for (int done = 0; done < pv.group; done += HEADS_PER_PASS) {
+    const int n = std::min(HEADS_PER_PASS, pv.group - done);
+    auto go = [&](auto kernel, unsigned waves, const auto& its) {
+      return launch(kernel, dim3(workgroups), 64 * waves, stream, done == 0 ? ev_start : nullptr, done + n >= pv.group ? ev_stop : nullptr, pv,
+                    (const uint16_t*)q, (const char*)k_new, (const char*)v_new, ws, (uint16_t*)out, scale_log2, (int32_t)done, (int32_t)n, its);
+    };
+    int e = -1;
+    if (a.step_units > STEP_UNITS) {
+      auto in_blocks = [&](const auto& its) {
+        using Its = std::decay_t<decltype(its)>;
+        if (a.step_units <= BLOCK_UNITS) return go(decode_fp4_block_kernel<D, 2, HEADS_PER_PASS, 8, APPEND, DIRECT, Its>, 8, its);
+        return go(decode_fp4_block_kernel<D, WIDE_UNITS / WIDE_WAVES, HEADS_PER_PASS, WIDE_WAVES, APPEND, DIRECT, Its>, WIDE_WAVES, its);
+      };
+      e = in_blocks(args);
+    } else {
+      if constexpr (!PAIR)               // (single_waves() is for several passes)
+        if (a.wg_waves == 1) e = go(decode_fp4_kernel<D, FP4_UNITS, HEADS_PER_PASS, 1, APPEND, DIRECT, Args>, 1, args);
+      if (e < 0) e = go(decode_fp4_kernel<D, FP4_UNITS, HEADS_PER_PASS, SHARE_WAVES, APPEND, DIRECT, Args>, SHARE_WAVES, args);
+    }
+    if (e) return e;
+  }
+  return 0;
+}
+
+template <class Args>
+static int launch_fp4(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
+                      const BatchArgs& a, const Args& args, unsigned workgroups, hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop) {
+  auto go = [&](auto launch) { return launch(pv, q, k_new, v_new, ws, out, scale_log2, a, args, workgroups, stream, ev_start, ev_stop); };
+  auto of_size = [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    if (k_new) return pv.vbase ? go(launch_fp4_i<D, true, true, Args>) : go(launch_fp4_i<D, true, false, Args>);
+    return pv.vbase ? go(launch_fp4_i<D, false, true, Args>) : go(launch_fp4_i<D, false, false, Args>);
+  };
+  return pv.head_dim == 128 ? of_size(std::integral_constant<int, 128>{}) : of_size(std::integral_constant<int, 64>{});
+}
+
+static unsigned workgroups_of(const PoolView& pv, const BatchArgs& a) {
+  return ((unsigned)(a.waves_per_head * pv.n_kv_heads) + a.wg_waves - 1) / a.wg_waves;
+}
+
+int launch_fp4_decode(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
+                      const BatchArgs& a, hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop) {
+  if (a.n_req <= 0 || a.waves_per_head <= 0) return 0;
+  return launch_fp4(pv, q, k_new, v_new, ws, out, scale_log2, a, a, workgroups_of(pv, a), stream, ev_start, ev_stop);
+}
+
+int launch_fp4_decode_pair(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
+                           PairArgs& a, hipStream_t stream, hipEvent_t ev_start, hipEvent_t ev_stop) {
+  a.workgroups = workgroups_of(pv, a.half[0]);
+  return launch_fp4(pv, q, k_new, v_new, ws, out, scale_log2, a.half[0], a, a.workgroups + workgroups_of(pv, a.half[1]), stream, ev_start, ev_stop);
+}
+
+}  // namespace ellm

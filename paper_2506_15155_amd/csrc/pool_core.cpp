@@ -431,6 +431,100 @@ int PoolCore::decode_check(const int32_t* ids, int32_t batch, int32_t extra) {
   return OK;
 }
 
+// the slots of tokens [first, end) have a device chunk each
+int PoolCore::resident(const int32_t* r, int64_t first, int64_t end, const char* unmapped, const char* on_host) {
+  if (first >= end) return OK;
+  for (int64_t s = first / g_.tokens_per_chunk; s <= (end - 1) / g_.tokens_per_chunk; s++) {
+    if (r[s] == ENTRY_UNMAPPED) return fail(ERR_UNMAPPED, unmapped);
+    if (r[s] <= -2) return fail(ERR_NOT_RESIDENT, on_host);
+  }
+  return OK;
+}
+
+// *n: how many tokens from `first` on are meant, all of them there
+int PoolCore::source_check(int32_t id, int64_t first, const int64_t* n_tokens, int64_t* n) {
+  const TensorRec* t = tensor(id);
+  if (!t) return fail(ERR_INVALID, "bad tensor handle");
+  if (first < 0 || (n_tokens && *n_tokens < 0)) return fail(ERR_INVALID, "negative position or token count");
+  if (first > t->len || (n_tokens && *n_tokens > t->len - first)) return fail(ERR_RANGE, "tokens past the end of the tensor");
+  *n = n_tokens ? *n_tokens : t->len - first;
+  return resident(row(id), first, first + *n, "slot of a token has no chunk", "slot of a token is in host memory");
+}
+
+int PoolCore::read_check(const int32_t* ids, int32_t batch, const int64_t* first, const int64_t* n_tokens, std::vector<int32_t>& n_eff,
+                         int64_t* total) {
+  if (batch < 0 || (batch > 0 && !ids)) return fail(ERR_INVALID, "kv_read: bad batch");
+  n_eff.resize(batch);
+  *total = 0;
+  for (int32_t b = 0; b < batch; b++) {
+    int64_t n = 0;
+    const int rc = source_check(ids[b], first ? first[b] : 0, n_tokens ? n_tokens + b : nullptr, &n);
+    if (rc) return rc;
+    n_eff[b] = (int32_t)n;
+    *total += n;
+  }
+  return OK;
+}
+
+int PoolCore::copy_check(const int32_t* src, const int32_t* dst, int32_t n, const int64_t* first, const int64_t* n_tokens,
+                         std::vector<int32_t>& n_eff, int64_t* total) {
+  if (n < 0 || (n > 0 && (!src || !dst))) return fail(ERR_INVALID, "kv_copy: bad count");
+  n_eff.resize(n);
+  *total = 0;
+  // handles are marked as destinations first, so that any order of the pairs finds one that is a source as well
+  ++stamp_now_;
+  for (int32_t i = 0; i < n; i++) {
+    if (!tensor(dst[i])) return fail(ERR_INVALID, "kv_copy: bad tensor handle");
+    if (stamp_[dst[i]] == stamp_now_) return fail(ERR_INVALID, "kv_copy: destination given twice");
+    stamp_[dst[i]] = stamp_now_;
+  }
+  for (int32_t i = 0; i < n; i++) {
+    int64_t m = 0;
+    int rc = source_check(src[i], first ? first[i] : 0, n_tokens ? n_tokens + i : nullptr, &m);
+    if (rc) return rc;
+    if (stamp_[src[i]] == stamp_now_) return fail(ERR_INVALID, "kv_copy: a tensor is source and destination");
+    const TensorRec* t = tensor(dst[i]);
+    if (m > t->max_tokens - t->len) return fail(ERR_RANGE, "kv_copy: tensor would exceed max_tokens");
+    if ((rc = resident(row(dst[i]), t->len, t->len + m, "kv_copy: target slot has no chunk", "kv_copy: target slot is in host memory"))) return rc;
+    n_eff[i] = (int32_t)m;
+    *total += m;
+  }
+  return OK;
+}
+
+int PoolCore::compact_check(const int32_t* ids, int32_t batch, const int64_t* first, const int64_t* n_keep, int64_t* total) {
+  if (batch < 0 || (batch > 0 && !ids)) return fail(ERR_INVALID, "kv_compact: bad batch");
+  *total = 0;
+  ++stamp_now_;
+  for (int32_t b = 0; b < batch; b++) {
+    const TensorRec* t = tensor(ids[b]);
+    if (!t) return fail(ERR_INVALID, "kv_compact: bad tensor handle");
+    if (stamp_[ids[b]] == stamp_now_) return fail(ERR_INVALID, "kv_compact: tensor handle given twice");
+    stamp_[ids[b]] = stamp_now_;
+    const int64_t f = first ? first[b] : 0, k = n_keep ? n_keep[b] : 0;
+    if (f < 0 || k < 0) return fail(ERR_INVALID, "kv_compact: negative position or token count");
+    if (f > t->len || k > t->len - f) return fail(ERR_RANGE, "kv_compact: more tokens than the tensor has");
+    if (k == 0) continue;
+    const int rc = resident(row(ids[b]), f, t->len, "kv_compact: slot of a token has no chunk", "kv_compact: slot of a token is in host memory");
+    if (rc) return rc;
+    *total += k;
+  }
+  return OK;
+}
+
+void PoolCore::compact_commit(const int32_t* ids, int32_t batch, const int64_t* first, const int64_t* n_keep, bool unmap) {
+  for (int32_t b = 0; b < batch; b++) {
+    TensorRec& t = t_[ids[b]];
+    t.len = (first ? first[b] : 0) + (n_keep ? n_keep[b] : 0);
+    if (!unmap) continue;
+    for (int64_t s = (t.len + g_.tokens_per_chunk - 1) / g_.tokens_per_chunk; s < t.n_slots; s++) {
+      if (row(ids[b])[s] == ENTRY_UNMAPPED) continue;
+      release_entry(row(ids[b])[s]);
+      set_entry(ids[b], (int32_t)s, ENTRY_UNMAPPED);
+    }
+  }
+}
+
 int PoolCore::offload_plan(int32_t id, int32_t first, int32_t n, std::vector<Move>& moves) {
   moves.clear();
   const TensorRec* t = tensor(id);

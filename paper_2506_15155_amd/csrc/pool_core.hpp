@@ -32,6 +32,7 @@ struct Geometry {
   int32_t n_chunks = 0, n_host_slots = 0, tokens_per_chunk = 0;
   uint32_t chunk_bytes = 0;
   int32_t n_q_heads = 0, n_kv_heads = 0, head_dim = 0, group = 0;
+  bool fp4 = false;        // rows are held in 4 bits (ELLM_MXFP4), else in bf16
   int32_t max_tensors = 0, max_slots = 0;
   uint64_t bytes_per_token = 0;
 };
@@ -82,6 +83,18 @@ class PoolCore {
   // extra: tokens a not yet committed append adds to every request (0 or 1)
   int decode_check(const int32_t* ids, int32_t batch, int32_t extra = 0);
 
+  // tokens first[i] .. of src[i] behind those of dst[i] (n_tokens NULL: all from there on; first NULL: from 0 on);
+  // on success n_eff[i] holds the token counts. commit adds them to the lengths of dst
+  int copy_check(const int32_t* src, const int32_t* dst, int32_t n, const int64_t* first, const int64_t* n_tokens,
+                 std::vector<int32_t>& n_eff, int64_t* total);
+  // tokens to be read out: as the sources of a copy
+  int read_check(const int32_t* ids, int32_t batch, const int64_t* first, const int64_t* n_tokens, std::vector<int32_t>& n_eff,
+                 int64_t* total);
+  // of every tensor's tokens the first `first` and n_keep of the others stay (either NULL: 0 each); total: of n_keep.
+  // commit sets the lengths and, with unmap, empties the slots behind them
+  int compact_check(const int32_t* ids, int32_t batch, const int64_t* first, const int64_t* n_keep, int64_t* total);
+  void compact_commit(const int32_t* ids, int32_t batch, const int64_t* first, const int64_t* n_keep, bool unmap);
+
   // offload / fetch: plan lists the moves in slot order; commit applies them
   int offload_plan(int32_t id, int32_t first, int32_t n, std::vector<Move>& moves);
   void offload_commit(int32_t id, const std::vector<Move>& moves);
@@ -123,6 +136,8 @@ class PoolCore {
   int32_t* row_mut(int32_t id) { return &table_[(size_t)id * g_.max_slots]; }
   void set_entry(int32_t id, int32_t slot, int32_t value);
   void release_entry(int32_t e);
+  int resident(const int32_t* row, int64_t first, int64_t end, const char* unmapped, const char* on_host);
+  int source_check(int32_t id, int64_t first, const int64_t* n_tokens, int64_t* n);
   int pick_chunks(int32_t n, const int32_t* explicit_ids, bool inflate, std::vector<int32_t>& out);
   void take_chunk(int32_t c, int32_t id, int32_t slot);
 
