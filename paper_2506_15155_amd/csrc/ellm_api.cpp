@@ -859,6 +859,10 @@ int ensure_workspace(ellm_pool* p, int64_t n_slots) {
 // every workload: the second wave of a SIMD gets its loads served 15 to 50 % more slowly than the
 // first, and it takes bandwidth from it. Without a device (metadata-only pools, planning calls on
 // a host without GPU) a nominal MI355X figure is used: 256 compute units x 4 SIMDs.
+int32_t waves_per_cu(const ellm_pool* p) {
+  if (p->geom.fp4) return ellm::fp4_waves_per_cu(p->geom.head_dim, p->geom.group);
+  return std::min(ellm::SIMDS_PER_CU, ellm::partial_waves_per_cu(p->geom.head_dim, p->geom.group, p->geom.tokens_per_chunk));
+}
 int32_t wave_slots(ellm_pool* p) {
   if (p->wave_slots > 0) return p->wave_slots;
   int32_t slots = 256 * ellm::SIMDS_PER_CU;
@@ -867,7 +871,7 @@ int32_t wave_slots(ellm_pool* p) {
     int dev = 0, cus = 0;
     if (hipGetDevice(&dev) == hipSuccess &&
         hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0) {
-      slots = cus * std::min(ellm::SIMDS_PER_CU, ellm::partial_waves_per_cu(p->geom.head_dim, p->geom.group, p->geom.tokens_per_chunk));
+      slots = cus * waves_per_cu(p);
       p->compute_units = cus;
     } else {
       (void)hipGetLastError();
@@ -1016,12 +1020,16 @@ void plan_launch(ellm_pool* p, const int32_t* ids, int32_t n_req, int32_t q_row0
     total = waves = blocks;
   } else {
     waves = std::max<int64_t>(1, std::min(room, total));
+    // 4-bit rows: several waves for every SIMD. The workspace's bound holds for them because partial results are counted by
+    // workgroup and a kv head's waves are whole workgroups: they have W / SHARE_WAVES - 1 boundaries, and one slot more than
+    // boundaries for every request that is split; steps, which may be any number, are as many as there are SIMDs.
+    if (p->geom.fp4 && waves >= ellm::SHARE_WAVES) waves -= waves % ellm::SHARE_WAVES;
     if (!tiles) {
       // The entry point with the fixed workspace takes every batch whose cut in 64-token pieces of a chunk
       // fits there; where that cut would fit and this one does not, it is made coarser until it does
       // (for both entry points, which share the cut).
       const int64_t cap = (int64_t)(ellm::STATIC_WS_BYTES / slot_bytes(p->geom.group, p->geom.head_dim)) / n_kv;
-      const bool by_steps = steps <= room;
+      const bool by_steps = steps <= (p->geom.fp4 ? std::min<int64_t>(room, cus * ellm::SIMDS_PER_CU / n_kv) : room);
       const int64_t need = by_steps ? step_parts : waves + n_req - 1 > cap ? cut_shares(units, total, waves, nullptr) : 0;
       bool coarser = false;
       if (need > cap) {
@@ -1033,6 +1041,7 @@ void plan_launch(ellm_pool* p, const int32_t* ids, int32_t n_req, int32_t q_row0
       }
       if (coarser) {
         while (waves > 1 && cut_shares(units, total, waves, nullptr) > cap) waves -= (waves + 15) / 16;
+        if (p->geom.fp4 && waves >= ellm::SHARE_WAVES) waves -= waves % ellm::SHARE_WAVES;
       } else if (by_steps) {
         a.step_units = ellm::STEP_UNITS;
         for (int32_t i = 0; i < n_req; i++) units[i] = (units[i] + ellm::STEP_UNITS - 1) / ellm::STEP_UNITS;
@@ -1044,7 +1053,7 @@ void plan_launch(ellm_pool* p, const int32_t* ids, int32_t n_req, int32_t q_row0
   const bool single = ellm::single_waves(p->geom.group, block_units > 0, total * a.step_units, waves, n_req);
   const int32_t merge_parts = single ? 0 : ellm::merge_parts(p->geom.head_dim, p->geom.group, block_units > 0, tiles);
   a.wg_waves = block_units || single ? 1 : ellm::SHARE_WAVES;
-  const int64_t parts = cut_shares(units, total, waves, &a, merge_parts);
+  int64_t parts = cut_shares(units, total, waves, &a, merge_parts);
   a.in_order_parts = block_units ? merge_parts : 0;
   a.n_req = n_req;
   a.q_row0 = q_row0;
@@ -1052,6 +1061,7 @@ void plan_launch(ellm_pool* p, const int32_t* ids, int32_t n_req, int32_t q_row0
   a.waves_per_head = (int32_t)std::min<int64_t>(waves, 0x7fffffff);
   a.parts_per_head = (int32_t)std::min<int64_t>(parts, 0x7fffffff);
   a.ws_slots = (int32_t)std::min<int64_t>(parts * n_kv, 0x7fffffff);
+  if (p->geom.fp4 && !block_units && p->split_override == 0 && p->waves_percent == 100) parts = ellm::slots_by_workgroup(a, n_kv);
   a.by_waves = ellm::divisor(a.waves_per_head);
   p->plan_total_units = total;
   p->plan_waves = waves;
@@ -1791,7 +1801,8 @@ int ellm_debug_set_compute_units(ellm_pool* p, int32_t n) {
   if (!p->metadata_only && n * ellm::SIMDS_PER_CU > device_simds())
     return set_err(ELLM_ERR_INVALID, "set_compute_units: more than the GPU has");
   p->compute_units = n;
-  p->wave_slots = n * ellm::SIMDS_PER_CU;      // 0: asked for again by the next plan
+  // 0: asked for again by the next plan
+  p->wave_slots = n * (p->geom.fp4 && !p->metadata_only ? waves_per_cu(p) : ellm::SIMDS_PER_CU);
   return ELLM_OK;
 }
 

@@ -333,6 +333,8 @@ int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const 
 
 // ---- rows in 4 bits (fp4.hpp) ----
 int launch_fp4_append(const PoolView& pv, const void* k_new, const void* v_new, const TokenArgs& a, hipStream_t stream);
+// waves of a compute unit that a launch which fills the GPU is cut for
+int fp4_waves_per_cu(int head_dim, int group);
 // as launch_decode_partial and launch_decode_pair; the combine pass is the same
 int launch_fp4_decode(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
                       const BatchArgs& a, hipStream_t stream, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);

@@ -11,10 +11,9 @@
 //      codes the conversion instruction turns into bf16 values, exactly, eight dims (a word) to an operand. The contraction
 //      index of lane group g is its own quarter of the dims; Q is laid out alike. Register i of a unit's result is the score
 //      of token 4 g + i for head c.
-//   softmax  a lane owns head c and four tokens of every unit; the weights are where the second product wants them, as the
-//      sum of two bf16 values (the next one below, and the rest), so they lose nothing that the result would show.
+//   softmax  a lane owns head c and four tokens of every unit; the weights are where the second product wants them.
 //   PV      O^T = V^T P^T, two units at a time: contraction index of lane group g = its four tokens of either unit. Lane l loads a
-//      quarter of row l / 4; as bf16 values with their scale on them the rows of two units go through LDS, which hands them
+//      quarter of row l / 4; as fp16 values with their scale on them the rows of two units go through LDS, which hands them
 //      out transposed (a read that gives a lane 4 rows of one dim).
 // Products in 4 and 8 bits with scales (16x16x128) would take the codes as they are, but do not add up in 32 bits: their results
 // were 8e-5 of the sum of the products' magnitudes off.
@@ -24,31 +23,55 @@
 namespace ellm {
 
 enum : uint32_t { T_FIRST = 1, T_LAST = 2, T_FIN = 4 };   // a tile starts a request here, ends it, ends the share
-template <int U>
-struct Fp4Tile {                     // what is known of a tile before its loads are issued (uniform)
+// What is known of a tile before its loads are issued (uniform). RUN: its units are neighbours in one chunk, a tile ends where its
+// chunk does, and one address is enough for all of it; else every unit has an address of its own.
+template <int U, bool RUN>
+struct Fp4Tile {
+  static constexpr int PIECES = RUN ? 1 : U;
   int32_t n, b, part;                // units, request, partial slot of the request in this wave (-1: finished here)
   uint32_t flags;                    // T_*
   int32_t tail;                      // rows of its last unit
-  int32_t nv[U];                     // rows of each unit (0: the tile has no such unit)
-  int32_t r[U];                      // first row of the unit in its chunk
-  uint32_t at[U];                    // its chunk (table entry, or slot of the tensor's own range)
+  int32_t rows[PIECES];              // of the run, or of each unit (0: the tile has no such unit)
+  int32_t r[PIECES];                 // first row in its chunk
+  uint32_t at[PIECES];               // the chunk (table entry, or slot of the tensor's own range)
   const char* base;                  // start of the pool, or of the tensor's range
 };
 
-// V rows of two units on their way through LDS: 32 bytes between rows keep the transposing reads off each other's banks
+// V rows of two units on their way through LDS. Rows are 32 bytes apart modulo the banks' 128, which keeps the transposing
+// reads (32 bytes of 4 rows at a time) off each other's banks, and the writes (16 bytes of all quarters of 2 rows) are kept apart by
+// 16 bytes between the halves of a row (heads of 128), or by the order of a quarter's 16 bytes in odd rows (heads of 64).
 template <int D> constexpr int STAGE_ROW = 2 * D + 32;
 template <int D> constexpr int STAGE_BYTES = 2 * UNIT_TOKENS * STAGE_ROW<D>;
+template <int D>
+__device__ __forceinline__ int32_t stage_write(int32_t row, int32_t quarter, int32_t w) {
+  if constexpr (D == 128) return row * STAGE_ROW<D> + quarter * 64 + (quarter >> 1) * 16 + w * 16;
+  else return row * STAGE_ROW<D> + quarter * 32 + ((w ^ (row & 1)) * 16);
+}
+// 4 dims, the fourth `piece`, of block n of 16 dims
+template <int D>
+__device__ __forceinline__ int32_t stage_read(int32_t row, int32_t piece, int32_t n) {
+  if constexpr (D == 128) return row * STAGE_ROW<D> + n * 32 + (n >> 2) * 16 + piece * 8;
+  else return row * STAGE_ROW<D> + n * 32 + ((piece * 8) ^ ((row & 1) * 16));
+}
+
+// The second product is one of fp16 values, of more bits than bf16 and a smaller range, which is used to its ends. A weight is held
+// relative to the running maximum, at most 2^WEIGHT_BITS; what its rounding loses is 2^-12 of it, or, of the smallest ones, 2^-25 of
+// 1 / 2^WEIGHT_BITS: 2^-37 of the largest weight. A scale of V is held relative to the largest one that the wave has met in the
+// request, and the values are exact down to 2^-36 of it. (Weights as sums of two bf16 values, which need no such care, take twice as
+// many products and 60 more of 310 instructions a tile: 16 requests of 32768 to 131072 tokens, 8 q heads each 249 us a call.)
+constexpr int WEIGHT_BITS = 12, VALUE_BITS = 13;
 
 typedef short __attribute__((ext_vector_type(4))) s16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 
 // NW == 0: a wave walks its share, SW of them are a workgroup (SW == 1: single_waves()). NW > 0: NW waves share a step of up to NW * U units
 // of one request, one tile each, and add up through LDS. HEADS: q heads that LDS has room for.
-template <int D, int U, int HEADS, bool APPEND, bool DIRECT, int NW, int SW, class Args>
+template <int D, int U, int HEADS, bool RUN, bool APPEND, bool DIRECT, int NW, int SW, class Args>
 __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new,
                                                 const char* __restrict__ v_new, float* __restrict__ ws, uint16_t* __restrict__ out,
                                                 float scale_log2, int32_t g_first, int32_t n_heads, const Args& a, int32_t workgroup) {
   constexpr int W = D / 32, ROW = FP4_ROW<D>, SCALES = FP4_SCALES<D>;     // words of a lane's quarter of a row
+  using Tile = Fp4Tile<U, RUN>;
   constexpr int NB = D / 16, F = D / 4;                                   // 16-dim blocks of the result; pieces of its rows
   static_assert(U % 2 == 0, "PV takes two units at a time");
   const int lane = threadIdx.x & 63, c = lane & 15, g16 = lane >> 4, vr = lane >> 2, vp = lane & 3;
@@ -66,6 +89,11 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   const int32_t hq0 = g * pv.group + g_first;        // first q head handled here
   const int32_t head = min(c, n_heads - 1);          // lanes beyond the last head repeat it and write nothing
   const uint64_t head_rows = (uint64_t)(2 * g) * plane, head_scales = fp4_scales_at<D>(pv) + (uint64_t)(2 * g) * scale_plane;
+
+  // Scores are kept without the scale, of which only the sign goes into the query (the maximum has to be one): its size is part
+  // of the exponential's argument, in log2 units, as are the maximum m and the other kernels' partial results.
+  const float size = __builtin_fabsf(scale_log2);
+  const uint32_t sign = scale_log2 < 0.f ? 0x80008000u : 0u;
 
   // ---- cursor: the next tile to be asked for ----
   int32_t cb = sh.b, rem_share = sh.n_units, len, slot, r, rem_req, part;
@@ -86,30 +114,42 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     r = (u0 - slot * pv.units_per_chunk) * UNIT_TOKENS;
     part = rq.n_part == 1 ? -1 : rq.part0 + (sh.w - rq.wave_first);    // (which slot: only where a workgroup is a step)
   }
-  auto advance = [&](Fp4Tile<U>& t) __attribute__((always_inline)) {
+  auto advance = [&](Tile& t) __attribute__((always_inline)) {
     t.n = min(U, min(rem_share, rem_req));
     t.b = cb;
     t.part = part;
     t.flags = first;
     t.base = DIRECT ? walk.tbase : pv.base;
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      if (u == 0 || u < t.n) {
-        t.at[u] = DIRECT ? (uint32_t)slot : (uint32_t)walk.trow[slot];
-        t.r[u] = r;
-        t.nv[u] = min(UNIT_TOKENS, min(Tc - r, len - (slot * Tc + r)));
-        t.tail = t.nv[u];
-        if (u < t.n - 1 || (t.n > 0 && rem_req > t.n)) {   // there is a next unit of this request
-          r += UNIT_TOKENS;
-          if (r >= Tc) { r = 0; slot += 1; }
-        }
-      } else {
-        t.at[u] = t.at[u - 1];
-        t.r[u] = t.r[u - 1];
-        t.nv[u] = 0;
+    if constexpr (RUN) {
+      t.n = min(t.n, (Tc - r + UNIT_TOKENS - 1) / UNIT_TOKENS);
+      t.at[0] = DIRECT ? (uint32_t)slot : (uint32_t)walk.trow[slot];
+      t.r[0] = r;
+      t.rows[0] = min(t.n * UNIT_TOKENS, min(Tc - r, len - (slot * Tc + r)));      // (past the end of the share: 0)
+      t.tail = t.rows[0] - (t.n - 1) * UNIT_TOKENS;
+      if (rem_req > t.n) {                             // there is a next unit of this request
+        r += t.n * UNIT_TOKENS;
+        if (r >= Tc) { r = 0; slot += 1; }
       }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        if (u == 0 || u < t.n) {
+          t.at[u] = DIRECT ? (uint32_t)slot : (uint32_t)walk.trow[slot];
+          t.r[u] = r;
+          t.rows[u] = min(UNIT_TOKENS, min(Tc - r, len - (slot * Tc + r)));
+          t.tail = t.rows[u];
+          if (u < t.n - 1 || (t.n > 0 && rem_req > t.n)) {   // there is a next unit of this request
+            r += UNIT_TOKENS;
+            if (r >= Tc) { r = 0; slot += 1; }
+          }
+        } else {
+          t.at[u] = t.at[u - 1];
+          t.r[u] = t.r[u - 1];
+          t.rows[u] = 0;
+        }
+      }
+      if (t.n == 0) t.rows[0] = 0;                     // past the end of the share
     }
-    if (t.n == 0) t.nv[0] = 0;                       // past the end of the share
     rem_req -= t.n;
     rem_share -= t.n;
     first = 0;
@@ -129,17 +169,25 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       part = rq.n_part == 1 ? -1 : rq.part0;
     }
   };
-  // a unit's K rows and scales (V's: plane, scale_plane further on)
-  auto rows_base = [&](const Fp4Tile<U>& t, int u) __attribute__((always_inline)) {
-    return const_cast<char*>(t.base) + (uint64_t)t.at[u] * pv.chunk_bytes + head_rows + (uint32_t)t.r[u] * ROW;
+  // a piece's K rows and scales (V's: plane, scale_plane further on)
+  auto rows_base = [&](const Tile& t, int i) __attribute__((always_inline)) {
+    return const_cast<char*>(t.base) + (uint64_t)t.at[i] * pv.chunk_bytes + head_rows + (uint32_t)t.r[i] * ROW;
   };
-  auto scales_base = [&](const Fp4Tile<U>& t, int u) __attribute__((always_inline)) {
-    return const_cast<char*>(t.base) + (uint64_t)t.at[u] * pv.chunk_bytes + head_scales + (uint32_t)t.r[u] * SCALES;
+  auto scales_base = [&](const Tile& t, int i) __attribute__((always_inline)) {
+    return const_cast<char*>(t.base) + (uint64_t)t.at[i] * pv.chunk_bytes + head_scales + (uint32_t)t.r[i] * SCALES;
   };
   // how many of the rows are in the chunk: all but the one that a fused append is about to put there
-  auto there = [&](const Fp4Tile<U>& t, int u) __attribute__((always_inline)) {
-    return t.nv[u] - (APPEND && (t.flags & T_LAST) && u == t.n - 1 ? 1 : 0);
+  auto there = [&](const Tile& t, int i) __attribute__((always_inline)) {
+    return t.rows[i] - (APPEND && (t.flags & T_LAST) && (RUN || i == t.n - 1) ? 1 : 0);
   };
+  // rows of unit u
+  auto rows_of = [&](const Tile& t, int u) __attribute__((always_inline)) {
+    return RUN ? min(t.rows[0] - u * UNIT_TOKENS, UNIT_TOKENS) : t.rows[RUN ? 0 : u];
+  };
+  // the last piece of a tile (a unit that the tile does not have has the address of the one before it), and which row of it is
+  // the tile's last
+  constexpr int LAST = Tile::PIECES - 1;
+  auto last_row = [&](const Tile& t) __attribute__((always_inline)) { return (RUN ? t.rows[0] : t.tail) - 1; };
 
   // ---- loads ----
   // Buffer loads with the unit's rows as their range: rows past its end, and units that the tile does not have, come back as
@@ -161,7 +209,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     }
     return x;
   };
-  auto new_row = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+  auto new_row = [&](const Tile& t) __attribute__((always_inline)) {
     return ((int64_t)(a.q_row0 + t.b) * pv.n_kv_heads + g) * (2 * D);
   };
   auto load_new = [&](const char* from, int32_t quarter, uint32_t (&x)[D / 8]) __attribute__((always_inline)) {
@@ -172,28 +220,36 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       x[4 * i] = w.x; x[4 * i + 1] = w.y; x[4 * i + 2] = w.z; x[4 * i + 3] = w.w;
     }
   };
-  auto issue_k = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+  // ask(rows, scales, u, rows before unit u in them) for every unit of a tile, whose rows are so many bytes behind K's
+  auto each_piece = [&](const Tile& t, uint32_t rows_off, uint32_t scales_off, auto ask) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < Tile::PIECES; i++) {
+      const int32_t n = there(t, i);
+      const auto rows = buffer_at(rows_base(t, i) + rows_off, n * ROW), scales = buffer_at(scales_base(t, i) + scales_off, n * SCALES);
+#pragma unroll
+      for (int u = RUN ? 0 : i; u < (RUN ? U : i + 1); u++) ask(rows, scales, u, RUN ? u * UNIT_TOKENS : 0);
+    }
+  };
+  auto issue_k = [&](const Tile& t) __attribute__((always_inline)) {
     if (t.flags & T_FIRST) {
       const gptr_t qp = (gptr_t)(q + ((int64_t)(a.q_row0 + t.b) * pv.n_q_heads + hq0 + head) * D) + g16 * (D / 2);
 #pragma unroll
-      for (int w = 0; w < W; w++) qr[w] = *(const __attribute__((address_space(1))) words4_t*)(qp + w * 16);
+      for (int w = 0; w < W; w++) qr[w] = *(const __attribute__((address_space(1))) words4_t*)(qp + w * 16) ^ sign;
     }
     if (APPEND && (t.flags & T_LAST)) load_new(k_new + new_row(t), g16, kn);
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int32_t rows = there(t, u);
-      k[u] = load_quarter(buffer_at(rows_base(t, u), rows * ROW), c * ROW + g16 * (4 * W));
-      ks[u] = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(scales_base(t, u), rows * SCALES), c * SCALES + g16 / scale_of_quarter, 0, CPOL_NT);
-    }
+    auto ask = [&](const __amdgpu_buffer_rsrc_t rows, const __amdgpu_buffer_rsrc_t scales, int u, int at) __attribute__((always_inline)) {
+      k[u] = load_quarter(rows, at * ROW + c * ROW + g16 * (4 * W));
+      ks[u] = __builtin_amdgcn_raw_buffer_load_b8(scales, at * SCALES + c * SCALES + g16 / scale_of_quarter, 0, CPOL_NT);
+    };
+    each_piece(t, 0, 0, ask);
   };
-  auto issue_v = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+  auto issue_v = [&](const Tile& t) __attribute__((always_inline)) {
     if (APPEND && (t.flags & T_LAST)) load_new(v_new + new_row(t), vp, vn);
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int32_t rows = there(t, u);
-      v[u] = load_quarter(buffer_at(rows_base(t, u) + plane, rows * ROW), lane * (4 * W));
-      vs[u] = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(scales_base(t, u) + scale_plane, rows * SCALES), vr * SCALES + vp / scale_of_quarter, 0, CPOL_NT);
-    }
+    auto ask = [&](const __amdgpu_buffer_rsrc_t rows, const __amdgpu_buffer_rsrc_t scales, int u, int at) __attribute__((always_inline)) {
+      v[u] = load_quarter(rows, at * ROW + lane * (4 * W));
+      vs[u] = __builtin_amdgcn_raw_buffer_load_b8(scales, at * SCALES + vr * SCALES + vp / scale_of_quarter, 0, CPOL_NT);
+    };
+    each_piece(t, plane, scale_plane, ask);
   };
   // A quarter of a new row in 4 bits; `partner`: the larger magnitude of this lane's and that of the lane that has the other half of a
   // block (heads of 64)
@@ -219,8 +275,9 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
 
   // ---- arithmetic ----
   float m = NEG_BIG, l = 0.f;
+  uint32_t largest = 0;                              // of V's scales in the request so far
   f32x4_t acc[NB], s[U];
-  auto scores = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+  auto scores = [&](const Tile& t) __attribute__((always_inline)) {
     if (APPEND && (t.flags & T_LAST)) {
       // the new token's K row takes the place of what the loads found there, and goes into the chunk (a unit that the tile
       // does not have has the address of the one before it)
@@ -238,7 +295,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
         for (int w = 0; w < W; w++) k[u].w[w] = mine ? codes.w[w] : k[u].w[w];
         ks[u] = mine ? scale : ks[u];
       }
-      if (c == rl) store_new(rows_base(t, U - 1), scales_base(t, U - 1), rl, g16, codes, scale);
+      if (c == rl) store_new(rows_base(t, LAST), scales_base(t, LAST), last_row(t), g16, codes, scale);
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
@@ -246,10 +303,10 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       const float scale = fp4_scale_float(ks[u]);
 #pragma unroll
       for (int w = 0; w < W; w++) d = mfma16(fp4_values(k[u].w[w], scale), qr[w], d);
-      s[u] = d * scale_log2;
+      s[u] = d;
     }
   };
-  auto weigh = [&](const Fp4Tile<U>& t, char* stage) __attribute__((always_inline)) {
+  auto weigh = [&](const Tile& t, char* stage) __attribute__((always_inline)) {
     if (t.flags & T_FIRST) {
       m = NEG_BIG;
       l = 0.f;
@@ -258,13 +315,13 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     }
     bool full = true;
 #pragma unroll
-    for (int u = 0; u < U; u++) full &= t.nv[u] == UNIT_TOKENS;
+    for (int i = 0; i < Tile::PIECES; i++) full &= t.rows[i] == (RUN ? U * UNIT_TOKENS : UNIT_TOKENS);
     if (!full) {
       // scores of rows that are not there
 #pragma unroll
       for (int u = 0; u < U; u++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) s[u][i] = 4 * g16 + i < t.nv[u] ? s[u][i] : -INFINITY;
+        for (int i = 0; i < 4; i++) s[u][i] = 4 * g16 + i < rows_of(t, u) ? s[u][i] : -INFINITY;
     }
     if (APPEND && (t.flags & T_LAST)) {
       // the new token's V row
@@ -279,12 +336,12 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
         for (int w = 0; w < W; w++) v[u].w[w] = mine ? codes.w[w] : v[u].w[w];
         vs[u] = mine ? scale : vs[u];
       }
-      if (vr == rl) store_new(rows_base(t, U - 1) + plane, scales_base(t, U - 1) + scale_plane, rl, vp, codes, scale);
+      if (vr == rl) store_new(rows_base(t, LAST) + plane, scales_base(t, LAST) + scale_plane, last_row(t), vp, codes, scale);
     }
     float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
     for (int u = 1; u < U; u++) mx = fmaxf(mx, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
-    const float mn = fmaxf(m, max_xor32(max_xor16(mx)));
+    const float mn = fmaxf(m, max_xor32(max_xor16(mx)) * size);
     if (__builtin_amdgcn_ballot_w64(mn > m)) {       // some head has a new maximum
       const float alpha = fast_exp2(m - mn);
       l *= alpha;
@@ -292,38 +349,55 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       for (int n = 0; n < NB; n++) acc[n] *= alpha;
       m = mn;
     }
+    // the largest of V's scales in this tile (a block that is NaN has none)
+    uint32_t top = 0;
+#pragma unroll
+    for (int u = 0; u < U; u++) top = max(top, vs[u] == FP4_SCALE_NAN ? 0u : vs[u]);
+    if ((t.flags & T_FIRST) || __builtin_amdgcn_ballot_w64(top > largest)) {
+      const uint32_t now = wave_max_u32(top), before = t.flags & T_FIRST ? now : largest;
+      largest = max(now, before);
+#pragma unroll
+      for (int n = 0; n < NB; n++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], (int)(before - largest));
+    }
+    const float below = WEIGHT_BITS - m;
 #pragma unroll
     for (int u = 0; u < U; u += 2) {
-      uint32_t pb[4], pr[4];
+      words4_t weights;
 #pragma unroll
       for (int h = 0; h < 4; h++) {
         const f32x4_t& x = s[u + h / 2];
-        const float p0 = fast_exp2(x[2 * (h & 1)] - m), p1 = fast_exp2(x[2 * (h & 1) + 1] - m);
+        const float p0 = fast_exp2(x[2 * (h & 1)] * size + below), p1 = fast_exp2(x[2 * (h & 1) + 1] * size + below);
         l += p0 + p1;
-        const uint32_t b0 = bf16_below(p0), b1 = bf16_below(p1);
-        pb[h] = __builtin_amdgcn_perm(b1, b0, 0x07060302);
-        pr[h] = pack_bf16(p0 - __uint_as_float(b0), p1 - __uint_as_float(b1));
+        weights[h] = pack_f16(p0, p1);
       }
       // rows of units u and u + 1 to LDS: row 16 j + vr, dims of quarter vp
 #pragma unroll
       for (int j = 0; j < 2; j++) {
-        const float scale = fp4_scale_float(vs[u + j]);
+        const uint32_t e = __builtin_elementwise_sub_sat(vs[u + j] + (127 + VALUE_BITS), largest);
+        const float scale = fp4_scale_float(vs[u + j] == FP4_SCALE_NAN ? FP4_SCALE_NAN : e);
 #pragma unroll
         for (int w = 0; w < W; w++)
-          *reinterpret_cast<words4_t*>(stage + (UNIT_TOKENS * j + vr) * STAGE_ROW<D> + vp * (D / 2) + w * 16) = fp4_values(v[u + j].w[w], scale);
+          *reinterpret_cast<words4_t*>(stage + UNIT_TOKENS * j * STAGE_ROW<D> + stage_write<D>(vr, vp, w)) = fp4_values_f16(v[u + j].w[w], scale);
       }
-      const words4_t weights = {pb[0], pb[1], pb[2], pb[3]}, rest = {pr[0], pr[1], pr[2], pr[3]};
       // a block of 16 dims: lane (g, c) addresses 4 dims of row 4 g + c / 4 and gets dim c of rows 4 g .. 4 g + 3
-      char* const from = stage + (4 * g16 + (c >> 2)) * STAGE_ROW<D> + (c & 3) * 8;
 #pragma unroll
       for (int n = 0; n < NB; n++) {
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + 32 * n)),
-                      hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + UNIT_TOKENS * STAGE_ROW<D> + 32 * n));
-        const words2_t l2 = __builtin_bit_cast(words2_t, lo), h2 = __builtin_bit_cast(words2_t, hi);
-        const words4_t va = {l2.x, l2.y, h2.x, h2.y};
-        acc[n] = mfma16(va, rest, mfma16(va, weights, acc[n]));
+        char* const from = stage + stage_read<D>(4 * g16 + (c >> 2), c & 3, n);
+        const words2_t lo = __builtin_bit_cast(words2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)from)),
+                       hi = __builtin_bit_cast(words2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + UNIT_TOKENS * STAGE_ROW<D>)));
+        acc[n] = mfma16_f16(words4_t{lo.x, lo.y, hi.x, hi.y}, weights, acc[n]);
       }
     }
+  };
+  // the sums as they are without `largest`, when a request or the share ends
+  auto whole = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < NB; n++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], (int)largest - (127 + VALUE_BITS));
+    m -= WEIGHT_BITS;                                // (what the weights are relative to)
   };
   // which piece of a row, in the order of partial_dim() for units, has dims 16 n + 4 g16 .. + 3
   auto piece = [&](int n) __attribute__((always_inline)) {
@@ -343,13 +417,14 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     __shared__ float2 ml[NW][HEADS];
     float* const mine = reinterpret_cast<float*>(lds[wave]);
     if (rem_share > 0) {
-      Fp4Tile<U> t;
+      Tile t;
       advance(t);
       issue_k(t);
       issue_v(t);
       __builtin_amdgcn_sched_barrier(0);
       scores(t);
       weigh(t, lds[wave]);
+      whole();
       const float L = add_xor32(add_xor16(l));
       if (c < n_heads) {
 #pragma unroll
@@ -400,7 +475,8 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   __shared__ __attribute__((aligned(16))) char stages[NW ? 1 : SW][NW ? 1 : STAGE_BYTES<D>];
   __shared__ __attribute__((aligned(16))) Results<D, SW == 1 ? 1 : HEADS> results;     // (SW == 1: not used)
   char* const stage = stages[NW ? 0 : wave];
-  auto finish = [&](const Fp4Tile<U>& t) __attribute__((always_inline)) {
+  auto finish = [&](const Tile& t) __attribute__((always_inline)) {
+    whole();
     const float L = add_xor32(add_xor16(l));
     if (c >= n_heads) return;
     if (t.part < 0) {
@@ -430,7 +506,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   // No exit before the round's last load (the share's last round asks for rows it does not use): what is in flight when a
   // tile is waited for is the same on every path, so the compiler counts the loads exactly.
   if (index < a.waves_per_head * pv.n_kv_heads) {
-    Fp4Tile<U> t, next;
+    Tile t, next;
     advance(t);
     issue_k(t);
     issue_v(t);
@@ -456,12 +532,12 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   if constexpr (SW > 1) end_shares<D, HEADS>(pv, ws, out, a, records, results, g_first, n_heads, workgroup, wave, lane);
 }
 
-template <int D, int U, int HEADS, int SW, bool APPEND, bool DIRECT, class Args>
+template <int D, int U, int HEADS, int SW, bool RUN, bool APPEND, bool DIRECT, class Args>
 __global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(2, 2))) void decode_fp4_kernel(
     PoolView pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new, const char* __restrict__ v_new,
     float* __restrict__ ws, uint16_t* __restrict__ out, float scale_log2, int32_t g_first, int32_t n_heads, Args a) {
   in_launch(pv, ws, a, [&](const PoolView& pv, float* ws, const auto& a, int32_t workgroup) __attribute__((always_inline)) {
-    decode_fp4_body<D, U, HEADS, APPEND, DIRECT, 0, SW>(pv, q, k_new, v_new, ws, out, scale_log2, g_first, n_heads, a, workgroup);
+    decode_fp4_body<D, U, HEADS, RUN, APPEND, DIRECT, 0, SW>(pv, q, k_new, v_new, ws, out, scale_log2, g_first, n_heads, a, workgroup);
   });
 }
 template <int D, int U, int HEADS, int NW, bool APPEND, bool DIRECT, class Args>
@@ -469,14 +545,33 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     PoolView pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new, const char* __restrict__ v_new,
     float* __restrict__ ws, uint16_t* __restrict__ out, float scale_log2, int32_t g_first, int32_t n_heads, Args a) {
   in_launch(pv, ws, a, [&](const PoolView& pv, float* ws, const auto& a, int32_t workgroup) __attribute__((always_inline)) {
-    decode_fp4_body<D, U, HEADS, APPEND, DIRECT, NW, 1>(pv, q, k_new, v_new, ws, out, scale_log2, g_first, n_heads, a, workgroup);
+    decode_fp4_body<D, U, HEADS, false, APPEND, DIRECT, NW, 1>(pv, q, k_new, v_new, ws, out, scale_log2, g_first, n_heads, a, workgroup);
   });
 }
 
 // ---------------------------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------------------------
-constexpr int FP4_UNITS = 4;         // units per tile
+#ifndef FP4_U
+#define FP4_U 4
+#endif
+#ifndef FP4_W
+#define FP4_W 8
+#endif
+constexpr int FP4_UNITS = FP4_U;         // units per tile
+constexpr int FP4_WAVES_PER_CU = FP4_W;
+
+#ifndef FP4_RUN
+#define FP4_RUN 256
+#endif
+static bool fp4_runs(int tokens_per_chunk) { return tokens_per_chunk >= FP4_RUN; }
+
+// calls go(heads that LDS has room for) for a pass over n of them
+template <class Go>
+static int for_heads(int n, Go go) {
+  if (n <= 4) return go(std::integral_constant<int, 4>{});
+  return n <= 8 ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, HEADS_PER_PASS>{});
+}
 
 // a: the plan, or one of the two in `args`, which run the same kernel; workgroups: of all of it
 template <int D, bool APPEND, bool DIRECT, class Args>
@@ -501,12 +596,30 @@ static int launch_fp4_i(const PoolView& pv, const void* q, const void* k_new, co
       e = in_blocks(args);
     } else {
       if constexpr (!PAIR)               // (single_waves() is for several passes)
-        if (a.wg_waves == 1) e = go(decode_fp4_kernel<D, FP4_UNITS, HEADS_PER_PASS, 1, APPEND, DIRECT, Args>, 1, args);
-      if (e < 0) e = go(decode_fp4_kernel<D, FP4_UNITS, HEADS_PER_PASS, SHARE_WAVES, APPEND, DIRECT, Args>, SHARE_WAVES, args);
+        if (a.wg_waves == 1) e = go(decode_fp4_kernel<D, FP4_UNITS, HEADS_PER_PASS, 1, false, APPEND, DIRECT, Args>, 1, args);
+      if (e < 0)
+        e = for_heads(std::min(HEADS_PER_PASS, pv.group), [&](auto heads) {
+          if (fp4_runs(pv.tokens_per_chunk)) return go(decode_fp4_kernel<D, FP4_UNITS, heads(), SHARE_WAVES, true, APPEND, DIRECT, Args>, SHARE_WAVES, args);
+          return go(decode_fp4_kernel<D, FP4_UNITS, heads(), SHARE_WAVES, false, APPEND, DIRECT, Args>, SHARE_WAVES, args);
+        });
     }
     if (e) return e;
   }
   return 0;
+}
+
+int fp4_waves_per_cu(int head_dim, int group) {
+  if (group > HEADS_PER_PASS) return SIMDS_PER_CU;     // (a wave may leave a partial result of its own: see single_waves())
+  int n = 0;
+  auto ask = [&](auto dim) {
+    return for_heads(group, [&](auto h) {
+      return (int)hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void*)decode_fp4_kernel<dim(), FP4_UNITS, h(), SHARE_WAVES, false, true, false, BatchArgs>,
+                                                               64 * SHARE_WAVES, 0);
+    });
+  };
+  const int e = head_dim == 128 ? ask(std::integral_constant<int, 128>{}) : ask(std::integral_constant<int, 64>{});
+  if (e || n < 1) n = 1;
+  return std::min(n * SHARE_WAVES, FP4_WAVES_PER_CU);
 }
 
 template <class Args>
