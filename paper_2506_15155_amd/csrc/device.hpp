@@ -453,7 +453,8 @@ __device__ __forceinline__ void leave_partial(const PoolView& pv, float* ws, con
 // request, four waves; two, two waves each; more, a wave each. (A piece is whole heads: their (m, l) pairs belong to it.) With one
 // wave for a request and branches around the parts of each sum: 48 requests of 6 q heads each 49.95 -> 49.3 us, 64 of 16
 // heads of 64 66.4 -> 65.7, chunks of 16 tokens 33.6 -> 33.3, the 8B-shaped step 1995 -> 1985.
-template <int D, int HEADS, class Args>
+// ONE, TWO: how many partial results a lane asks for at a time where it adds up one column, or two.
+template <int D, int HEADS, int ONE = 16, int TWO = 8, class Args>
 __device__ __forceinline__ void end_shares(const PoolView& pv, float* ws_, uint16_t* __restrict__ out, const Args& a, const Records<Args>& records,
                                            const Results<D, HEADS>& res, int32_t g_first, int32_t n_heads, int32_t workgroup, int32_t wave, int32_t lane) {
   constexpr int F = D / 4, SLOTS = Results<D, HEADS>::SLOTS, NONE = Results<D, HEADS>::NONE;
@@ -528,12 +529,12 @@ __device__ __forceinline__ void end_shares(const PoolView& pv, float* ws_, uint1
     const int32_t x = h0 * F + lane;
     if ((h1 - h0) * F <= 64) {
       Sum s[1];
-      all.template sum<1, 4, 16>(s, x, 0, 0, parts.n);
+      all.template sum<1, 4, ONE>(s, x, 0, 0, parts.n);
       done(x, s[0]);
     } else {
       for (int32_t at = x; at - lane < h1 * F; at += 128) {
         Sum s[2];
-        all.template sum<2, 4, 8>(s, at, 64, 0, parts.n);
+        all.template sum<2, 4, TWO>(s, at, 64, 0, parts.n);
         done(at, s[0]);
         done(at + 64, s[1]);
       }

@@ -1082,6 +1082,7 @@ bool pair_up(ellm_pool* p, int64_t cap) {
     return a.unit_tokens == TILE_TOKENS ? 0 : a.step_units <= ellm::STEP_UNITS ? 1 : a.step_units <= ellm::BLOCK_UNITS ? 2 : 3;
   };
   if (kernel(p->launches[0]) != kernel(p->launches[1])) return false;
+  if (p->geom.fp4 && ellm::fp4_short_shares(p->geom.head_dim, p->launches[0]) != ellm::fp4_short_shares(p->geom.head_dim, p->launches[1])) return false;
   ellm::PairArgs& a = p->pair;
   int64_t slots[2];
   for (int i = 0; i < 2; i++) {

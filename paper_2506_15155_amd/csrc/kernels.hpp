@@ -333,6 +333,12 @@ int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const 
 
 // ---- rows in 4 bits (fp4.hpp) ----
 int launch_fp4_append(const PoolView& pv, const void* k_new, const void* v_new, const TokenArgs& a, hipStream_t stream);
+// Chunks of so many tokens and more are walked in runs of neighbouring units, whose loads need one address; tiles then end where
+// a chunk does. us a call by runs / with an address for every unit: 64 requests of 64 to 8192 tokens, 4 q heads each 22.0 / 23.2, 16 of
+// 32768 to 131072 250 / 268, 64 of 512 to 24576, 16 q heads of 64 32.2 / 38.3 (chunks of 1920 and 15408 tokens).
+constexpr int FP4_RUN_TOKENS = 256;
+// shares that are walked in smaller tiles (for why see kernels_fp4.hip)
+inline bool fp4_short_shares(int head_dim, const BatchArgs& a) { return head_dim == 128 && a.units_each * a.step_units < 20; }
 // waves of a compute unit that a launch which fills the GPU is cut for
 int fp4_waves_per_cu(int head_dim, int group);
 // as launch_decode_partial and launch_decode_pair; the combine pass is the same

@@ -37,21 +37,14 @@ struct Fp4Tile {
   const char* base;                  // start of the pool, or of the tensor's range
 };
 
-// V rows of two units on their way through LDS. Rows are 32 bytes apart modulo the banks' 128, which keeps the transposing
-// reads (32 bytes of 4 rows at a time) off each other's banks, and the writes (16 bytes of all quarters of 2 rows) are kept apart by
-// 16 bytes between the halves of a row (heads of 128), or by the order of a quarter's 16 bytes in odd rows (heads of 64).
-template <int D> constexpr int STAGE_ROW = 2 * D + 32;
-template <int D> constexpr int STAGE_BYTES = 2 * UNIT_TOKENS * STAGE_ROW<D>;
-template <int D>
-__device__ __forceinline__ int32_t stage_write(int32_t row, int32_t quarter, int32_t w) {
-  if constexpr (D == 128) return row * STAGE_ROW<D> + quarter * 64 + (quarter >> 1) * 16 + w * 16;
-  else return row * STAGE_ROW<D> + quarter * 32 + ((w ^ (row & 1)) * 16);
-}
-// 4 dims, the fourth `piece`, of block n of 16 dims
-template <int D>
-__device__ __forceinline__ int32_t stage_read(int32_t row, int32_t piece, int32_t n) {
-  if constexpr (D == 128) return row * STAGE_ROW<D> + n * 32 + (n >> 2) * 16 + piece * 8;
-  else return row * STAGE_ROW<D> + n * 32 + ((piece * 8) ^ ((row & 1) * 16));
+// V rows of two units on their way through LDS, half of the dims at a time (heads of 64: all): two words, 16 dims, of every quarter.
+// Rows are 32 bytes apart modulo the banks' 128, which keeps the transposing reads (32 bytes of 4 rows at a time) off each
+// other's banks; the order of a quarter's two words in odd rows keeps the writes (16 bytes of all quarters of 2 rows) apart.
+constexpr int STAGE_ROW = 4 * 32 + 32, STAGE_BYTES = 2 * UNIT_TOKENS * STAGE_ROW;
+__device__ __forceinline__ int32_t stage_write(int32_t row, int32_t quarter, int32_t w) { return row * STAGE_ROW + quarter * 32 + ((w ^ (row & 1)) * 16); }
+// 4 dims, the fourth `piece`, of the 16 of a quarter
+__device__ __forceinline__ int32_t stage_read(int32_t row, int32_t piece, int32_t quarter) {
+  return row * STAGE_ROW + quarter * 32 + ((piece * 8) ^ ((row & 1) * 16));
 }
 
 // The second product is one of fp16 values, of more bits than bf16 and a smaller range, which is used to its ends. A weight is held
@@ -372,22 +365,29 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
         l += p0 + p1;
         weights[h] = pack_f16(p0, p1);
       }
-      // rows of units u and u + 1 to LDS: row 16 j + vr, dims of quarter vp
+      float scale[2];
 #pragma unroll
       for (int j = 0; j < 2; j++) {
         const uint32_t e = __builtin_elementwise_sub_sat(vs[u + j] + (127 + VALUE_BITS), largest);
-        const float scale = fp4_scale_float(vs[u + j] == FP4_SCALE_NAN ? FP4_SCALE_NAN : e);
-#pragma unroll
-        for (int w = 0; w < W; w++)
-          *reinterpret_cast<words4_t*>(stage + UNIT_TOKENS * j * STAGE_ROW<D> + stage_write<D>(vr, vp, w)) = fp4_values_f16(v[u + j].w[w], scale);
+        scale[j] = fp4_scale_float(vs[u + j] == FP4_SCALE_NAN ? FP4_SCALE_NAN : e);
       }
-      // a block of 16 dims: lane (g, c) addresses 4 dims of row 4 g + c / 4 and gets dim c of rows 4 g .. 4 g + 3
 #pragma unroll
-      for (int n = 0; n < NB; n++) {
-        char* const from = stage + stage_read<D>(4 * g16 + (c >> 2), c & 3, n);
-        const words2_t lo = __builtin_bit_cast(words2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)from)),
-                       hi = __builtin_bit_cast(words2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + UNIT_TOKENS * STAGE_ROW<D>)));
-        acc[n] = mfma16_f16(words4_t{lo.x, lo.y, hi.x, hi.y}, weights, acc[n]);
+      for (int half = 0; half < W / 2; half++) {
+        // rows of units u and u + 1 to LDS: row 16 j + vr, words of quarter vp
+#pragma unroll
+        for (int j = 0; j < 2; j++)
+#pragma unroll
+          for (int w = 0; w < 2; w++)
+            *reinterpret_cast<words4_t*>(stage + stage_write(UNIT_TOKENS * j + vr, vp, w)) = fp4_values_f16(v[u + j].w[2 * half + w], scale[j]);
+        // 16 dims of a quarter: lane (g, c) addresses 4 of them in row 4 g + c / 4 and gets the c-th of rows 4 g .. 4 g + 3
+#pragma unroll
+        for (int p = 0; p < 4; p++) {
+          char* const from = stage + stage_read(4 * g16 + (c >> 2), c & 3, p);
+          const words2_t lo = __builtin_bit_cast(words2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)from)),
+                         hi = __builtin_bit_cast(words2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(from + UNIT_TOKENS * STAGE_ROW)));
+          const int n = p * (W / 2) + half;
+          acc[n] = mfma16_f16(words4_t{lo.x, lo.y, hi.x, hi.y}, weights, acc[n]);
+        }
       }
     }
   };
@@ -412,7 +412,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   if constexpr (NW > 0) {
     constexpr int ROWF = D + 4;                        // a row of a head's accumulators, padded against bank conflicts
     // a wave's V rows on their way through LDS, and then its sums
-    constexpr int MINE = std::max<int>(STAGE_BYTES<D>, HEADS * ROWF * 4);
+    constexpr int MINE = std::max<int>(STAGE_BYTES, HEADS * ROWF * 4);
     __shared__ __attribute__((aligned(16))) char lds[NW][MINE];
     __shared__ float2 ml[NW][HEADS];
     float* const mine = reinterpret_cast<float*>(lds[wave]);
@@ -472,7 +472,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     if (x < n_cols) write_out<D>(pv, out, a, cb, g, g_first, x, all_of[0]);
     return;
   }
-  __shared__ __attribute__((aligned(16))) char stages[NW ? 1 : SW][NW ? 1 : STAGE_BYTES<D>];
+  __shared__ __attribute__((aligned(16))) char stages[NW ? 1 : SW][NW ? 1 : STAGE_BYTES];
   __shared__ __attribute__((aligned(16))) Results<D, SW == 1 ? 1 : HEADS> results;     // (SW == 1: not used)
   char* const stage = stages[NW ? 0 : wave];
   auto finish = [&](const Tile& t) __attribute__((always_inline)) {
@@ -529,7 +529,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   } else if constexpr (SW > 1) {
     results.clear(wave, lane);
   }
-  if constexpr (SW > 1) end_shares<D, HEADS>(pv, ws, out, a, records, results, g_first, n_heads, workgroup, wave, lane);
+  if constexpr (SW > 1) end_shares<D, HEADS, 8, 4>(pv, ws, out, a, records, results, g_first, n_heads, workgroup, wave, lane);
 }
 
 template <int D, int U, int HEADS, int SW, bool RUN, bool APPEND, bool DIRECT, class Args>
@@ -552,19 +552,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // ---------------------------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------------------------
-#ifndef FP4_U
-#define FP4_U 4
-#endif
-#ifndef FP4_W
-#define FP4_W 8
-#endif
-constexpr int FP4_UNITS = FP4_U;         // units per tile
-constexpr int FP4_WAVES_PER_CU = FP4_W;
-
-#ifndef FP4_RUN
-#define FP4_RUN 256
-#endif
-static bool fp4_runs(int tokens_per_chunk) { return tokens_per_chunk >= FP4_RUN; }
+// Units per tile of heads of 128 in short shares, and of all others. Of shares of few tiles those count whose last tile, or the
+// last of a request, is not full; of long ones the bytes on their way. 64 requests of 64 to 8192 tokens, 8 kv heads (15 units a
+// wave) 19.9 us a call by 2 units, 20.8 by 4; 48, 6 q heads each 22.3, 24.6; chunks of 16 tokens 15.5, 17.0; 200 requests (28 units) 52.3,
+// 52.4; 32 of 2048 to 16384, 40 heads 268, 251; 16 of 32768 to 131072 241, 228. Heads of 64, 16 q heads, 64 of 512 to 24576 34.8, 30.5.
+constexpr int FP4_SHORT_TILE = 2, FP4_TILE = 4;
+// Two workgroups of four waves for every CU where LDS has room for them: one wave a SIMD 343 us, two 228 (16 requests of 32768 to
+// 131072 tokens, 8 q heads each); three and four, of smaller tiles, are no faster.
+constexpr int FP4_WAVES_PER_CU = 2 * SHARE_WAVES;
 
 // calls go(heads that LDS has room for) for a pass over n of them
 template <class Go>
@@ -596,11 +591,17 @@ static int launch_fp4_i(const PoolView& pv, const void* q, const void* k_new, co
       e = in_blocks(args);
     } else {
       if constexpr (!PAIR)               // (single_waves() is for several passes)
-        if (a.wg_waves == 1) e = go(decode_fp4_kernel<D, FP4_UNITS, HEADS_PER_PASS, 1, false, APPEND, DIRECT, Args>, 1, args);
+        if (a.wg_waves == 1) e = go(decode_fp4_kernel<D, FP4_TILE, HEADS_PER_PASS, 1, false, APPEND, DIRECT, Args>, 1, args);
       if (e < 0)
         e = for_heads(std::min(HEADS_PER_PASS, pv.group), [&](auto heads) {
-          if (fp4_runs(pv.tokens_per_chunk)) return go(decode_fp4_kernel<D, FP4_UNITS, heads(), SHARE_WAVES, true, APPEND, DIRECT, Args>, SHARE_WAVES, args);
-          return go(decode_fp4_kernel<D, FP4_UNITS, heads(), SHARE_WAVES, false, APPEND, DIRECT, Args>, SHARE_WAVES, args);
+          auto in_tiles = [&](auto units) {
+            if (pv.tokens_per_chunk >= FP4_RUN_TOKENS)
+              return go(decode_fp4_kernel<D, units(), heads(), SHARE_WAVES, true, APPEND, DIRECT, Args>, SHARE_WAVES, args);
+            return go(decode_fp4_kernel<D, units(), heads(), SHARE_WAVES, false, APPEND, DIRECT, Args>, SHARE_WAVES, args);
+          };
+          if constexpr (D == 128)
+            if (fp4_short_shares(D, a)) return in_tiles(std::integral_constant<int, FP4_SHORT_TILE>{});
+          return in_tiles(std::integral_constant<int, FP4_TILE>{});
         });
     }
     if (e) return e;
@@ -613,7 +614,7 @@ int fp4_waves_per_cu(int head_dim, int group) {
   int n = 0;
   auto ask = [&](auto dim) {
     return for_heads(group, [&](auto h) {
-      return (int)hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void*)decode_fp4_kernel<dim(), FP4_UNITS, h(), SHARE_WAVES, false, true, false, BatchArgs>,
+      return (int)hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void*)decode_fp4_kernel<dim(), FP4_TILE, h(), SHARE_WAVES, false, true, false, BatchArgs>,
                                                                64 * SHARE_WAVES, 0);
     });
   };
