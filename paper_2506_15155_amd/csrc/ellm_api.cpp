@@ -1444,9 +1444,12 @@ int ellm_kv_compact(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, cons
   }
   if ((rc = enter_compute(p, stream, ids, batch, 0))) return rc;
   int64_t key0 = 0;
+  const int32_t rows = ellm::compact_rows_per_segment(p->geom.head_dim, p->geom.fp4);
+  // counters and flags are in the workspace of partial results, which the calls of a pool use one after the other
+  const size_t n_marks = (size_t)p->ws_cap_slots * slot_bytes(p->geom.group, p->geom.head_dim) / sizeof(uint32_t);
   rc = in_groups(p, ids, batch, stream, "kv_compact launch", [&](int32_t b0, int32_t nb) {
     ellm::CompactArgs a;
-    a.n_req = 0;
+    a.n_req = a.segments = 0;
     int64_t in_group = 0;
     for (int32_t i = b0; i < b0 + nb; i++) {
       if (n_keep[i] == 0) continue;
@@ -1454,13 +1457,15 @@ int ellm_kv_compact(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, cons
       a.first[a.n_req] = first ? (int32_t)first[i] : 0;
       a.n[a.n_req] = (int32_t)n_keep[i];
       a.key0[a.n_req] = (int32_t)in_group;
-      a.len[a.n_req++] = (int32_t)p->core->tensor(ids[i])->len;
+      a.len[a.n_req] = (int32_t)p->core->tensor(ids[i])->len;
+      a.segment0[a.n_req++] = a.segments;
+      a.segments += (int32_t)((n_keep[i] + rows - 1) / rows);
       in_group += n_keep[i];
     }
     const int32_t* list = keep + key0;
     key0 += in_group;
     if (!a.n_req) return LAUNCH_NOTHING;
-    return ellm::launch_compact(view_of(p), p->geom.fp4, list, a, stream);
+    return ellm::launch_compact(view_of(p), p->geom.fp4, list, (uint32_t*)p->d_ws, n_marks, a, stream);
   }, [&](int32_t, int32_t) {});
   // the lengths and slots of the groups that were launched, behind the note of which chunks they touch
   const int32_t done = p->groups_done;

@@ -181,14 +181,18 @@ struct alignas(64) CopyTokenArgs {
 
 // Tokens that move together: of request b, the tokens at keep[key0[b] + i] become tokens first[b] + i, i < n[b]; keep (device
 // memory) ascends, so none moves up. len: tokens that are there.
+constexpr int COMPACT_BYTES = 64 << 10;     // of rows that a workgroup moves at a time: a segment
 struct alignas(64) CompactArgs {
-  int32_t n_req;
+  int32_t n_req, segments;         // segments of all requests, for one kv head's K (or V)
   int32_t tensor[MAX_LAUNCH_REQ];
   int32_t first[MAX_LAUNCH_REQ];
   int32_t n[MAX_LAUNCH_REQ];
   int32_t key0[MAX_LAUNCH_REQ];
   int32_t len[MAX_LAUNCH_REQ];
+  int32_t segment0[MAX_LAUNCH_REQ];// segments of the requests before this one
 };
+// words that a launch with chains of several segments counts and flags in: a line for each chain, a word for each segment
+inline size_t compact_marks(const CompactArgs& a, size_t chains) { return chains * ((size_t)a.n_req * MERGE_STRIDE + (size_t)a.segments); }
 
 struct PatchArgs {
   int32_t n;
@@ -352,7 +356,9 @@ int launch_read_tokens(const PoolView& pv, bool fp4, void* k_out, void* v_out, c
 // tokens of a workgroup's block
 int copy_tokens_per_block(int head_dim, bool fp4);
 int launch_copy_tokens(const PoolView& pv, bool fp4, const CopyTokenArgs& a, hipStream_t stream);
-int launch_compact(const PoolView& pv, bool fp4, const int32_t* keep, const CompactArgs& a, hipStream_t stream);
+// marks: room for n_marks words, which the launch clears itself; without enough of them chains go one segment after the other
+int compact_rows_per_segment(int head_dim, bool fp4);
+int launch_compact(const PoolView& pv, bool fp4, const int32_t* keep, uint32_t* marks, size_t n_marks, const CompactArgs& a, hipStream_t stream);
 
 // Device address and size of the library's fixed workspace on the current device (resolved once per
 // device, kept afterwards). Allocates nothing. Returns 0 or a hipError_t value.

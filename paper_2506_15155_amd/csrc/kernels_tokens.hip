@@ -189,29 +189,52 @@ __global__ __launch_bounds__(256) void copy_tokens_kernel(PoolView pv, CopyToken
 }
 
 // ---------------------------------------------------------------------------------------------
-// Compacting, in place: one workgroup for every (request, kv head, plane), which takes its kept rows STEP at a time, in
-// order. Step t writes rows [t STEP, (t + 1) STEP) of the moved part; what later steps read lies at (t + 1) STEP or behind it,
-// because positions ascend, and what earlier steps read has been read. So a step's rows have to be in registers before any
-// of them is stored, and nothing else. A position is held between its target and the tensor's last token: whatever the
-// list holds, no row outside the tensor's tokens is touched.
+// Compacting, in place. The moved rows of a (request, kv head, plane), a chain, are cut into segments of STEP rows, which a
+// workgroup holds in registers: it reads them where they are, and stores them where they go. Positions ascend, so what a
+// segment stores may only be what itself and segments before it read: a segment's stores wait until those before it that
+// read so far down have what they read in registers, which they say with a flag each, and wait for nothing else.
+// The segments of a chain are numbered in the order in which their workgroups begin (a counter for each chain), so whoever is
+// waited for is running already and does not wait itself: the launch comes to its end whatever order workgroups are started in.
+// A position is held between its target and the tensor's last token: whatever the list holds, no row outside the tensor's tokens
+// is touched.
+//
+// Chains of one segment need no flags and no counters. Where there is no room for flags (ONE_BY_ONE) a workgroup takes the segments
+// of its chain one after the other. us a call that way / with flags: 8 requests of 4096 to 16384 bf16 tokens, four fifths of them kept, 8
+// kv heads of 128 (240 MB read and written, 77 at a copy's rate) 446 / 106, one of 32768, half of them kept 587 / 37, in 4 bits 151 / 18.
+// A segment of 16 KB and 256 threads 159, 54, 20, of 32 and 512 125, 42, 19, of 64 and 1024 (taken) 106, 37, 18, of 128 and 1024 103, 30, 23;
+// 64 requests of 500 to 4000 4-bit tokens 72, 67, 69, 73. Without the streaming hints on loads and stores 152, 58, 28.
 // ---------------------------------------------------------------------------------------------
-template <int D, bool FP4, bool DIRECT>
-__global__ __launch_bounds__(512) void compact_kernel(PoolView pv, const int32_t* __restrict__ keep, CompactArgs a) {
+template <int D, bool FP4> constexpr int COMPACT_ROWS = COMPACT_BYTES / Rows<D, FP4>::BYTES;
+constexpr int COMPACT_THREADS = 1024;
+
+template <int D, bool FP4, bool DIRECT, bool ONE_BY_ONE>
+__global__ __launch_bounds__(COMPACT_THREADS) void compact_kernel(PoolView pv, const int32_t* __restrict__ keep, uint32_t* __restrict__ marks, CompactArgs a) {
   using R = Rows<D, FP4>;
-  constexpr int N = 4, STEP = N * 512 / R::LPR;
-  const int32_t b = blockIdx.x, h = blockIdx.y >> 1, plane = blockIdx.y & 1, sub = threadIdx.x % R::LPR;
-  const Tensor<DIRECT> t(pv, a.tensor[b]);
-  const int32_t n = a.n[b], first = a.first[b], last = a.len[b] - 1;
-  const int32_t* list = keep + a.key0[b];
+  constexpr int STEP = COMPACT_ROWS<D, FP4>, N = COMPACT_BYTES / (16 * COMPACT_THREADS), RPT = COMPACT_THREADS / R::LPR;     // rows of all threads at a time
+  constexpr int NS = FP4 ? (STEP + COMPACT_THREADS - 1) / COMPACT_THREADS : 1;
   using scales_t = std::conditional_t<R::SCALES == 4, uint32_t, uint16_t>;
-  constexpr int NS = FP4 ? STEP / 512 : 1;
-  for (int32_t i0 = 0; i0 < n; i0 += STEP) {
+  const int32_t b = ONE_BY_ONE ? blockIdx.x : find_last(a.segment0, a.n_req, blockIdx.x);
+  const int32_t h = blockIdx.y >> 1, plane = blockIdx.y & 1, sub = threadIdx.x % R::LPR;
+  const Tensor<DIRECT> t(pv, a.tensor[b]);
+  const int32_t n = a.n[b], first = a.first[b], last = a.len[b] - 1, segments = (n + STEP - 1) / STEP;
+  const int32_t* list = keep + a.key0[b];
+  auto source = [&](int32_t i) __attribute__((always_inline)) { return max(first + i, min(list[i], last)); };
+
+  __shared__ int32_t number;
+  uint32_t* const flags = marks + gridDim.y * a.n_req * MERGE_STRIDE + (ONE_BY_ONE ? 0 : gridDim.y * a.segment0[b] + blockIdx.y * segments);
+  int32_t seg = 0;
+  if (!ONE_BY_ONE && segments > 1) {
+    if (threadIdx.x == 0) number = (int32_t)atomicAdd(marks + (gridDim.y * b + blockIdx.y) * MERGE_STRIDE, 1u);
+    __syncthreads();
+    seg = number;
+  }
+  do {
+    const int32_t i0 = seg * STEP;
     uint4 x[N];
     scales_t scales[NS];
-    auto source = [&](int32_t i) __attribute__((always_inline)) { return max(first + i, min(list[i], last)); };
 #pragma unroll
     for (int j = 0; j < N; j++) {
-      const int32_t i = i0 + threadIdx.x / R::LPR + j * (512 / R::LPR);
+      const int32_t i = i0 + threadIdx.x / R::LPR + j * RPT;
       if (i >= n) continue;
       const RowAt at = t.row(pv, source(i));
       x[j] = load_stream16(at.chunk + R::rows_at(pv, h, plane) + at.row * R::BYTES + sub * 16);
@@ -219,17 +242,25 @@ __global__ __launch_bounds__(512) void compact_kernel(PoolView pv, const int32_t
     if constexpr (FP4) {
 #pragma unroll
       for (int j = 0; j < NS; j++) {
-        const int32_t i = i0 + threadIdx.x + j * 512;
-        if (i >= n) continue;
+        const int32_t i = i0 + threadIdx.x + j * COMPACT_THREADS;
+        if (i >= n || threadIdx.x + j * COMPACT_THREADS >= STEP) continue;
         const RowAt at = t.row(pv, source(i));
         scales[j] = *reinterpret_cast<const scales_t*>(at.chunk + R::scales_at(pv, h, plane) + at.row * R::SCALES);
       }
     }
     stores_done();               // (and loads: all that this wave has asked for is here)
     __syncthreads();
+    if (!ONE_BY_ONE && segments > 1) {
+      if (threadIdx.x == 0) __hip_atomic_store(flags + seg, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // the segments before this one that read as far as this one stores
+      for (int32_t j = threadIdx.x; j < seg; j += COMPACT_THREADS)
+        if (source((j + 1) * STEP - 1) >= first + i0)
+          while (!__hip_atomic_load(flags + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) __builtin_amdgcn_s_sleep(1);
+      __syncthreads();
+    }
 #pragma unroll
     for (int j = 0; j < N; j++) {
-      const int32_t i = i0 + threadIdx.x / R::LPR + j * (512 / R::LPR);
+      const int32_t i = i0 + threadIdx.x / R::LPR + j * RPT;
       if (i >= n) continue;
       const RowAt at = t.row(pv, first + i);
       store_stream16(at.chunk + R::rows_at(pv, h, plane) + at.row * R::BYTES + sub * 16, x[j]);
@@ -237,13 +268,14 @@ __global__ __launch_bounds__(512) void compact_kernel(PoolView pv, const int32_t
     if constexpr (FP4) {
 #pragma unroll
       for (int j = 0; j < NS; j++) {
-        const int32_t i = i0 + threadIdx.x + j * 512;
-        if (i >= n) continue;
+        const int32_t i = i0 + threadIdx.x + j * COMPACT_THREADS;
+        if (i >= n || threadIdx.x + j * COMPACT_THREADS >= STEP) continue;
         const RowAt at = t.row(pv, first + i);
         *reinterpret_cast<scales_t*>(at.chunk + R::scales_at(pv, h, plane) + at.row * R::SCALES) = scales[j];
       }
     }
-  }
+    seg++;
+  } while (ONE_BY_ONE && seg < segments);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -284,10 +316,24 @@ int launch_copy_tokens(const PoolView& pv, bool fp4, const CopyTokenArgs& a, hip
   });
 }
 
-int launch_compact(const PoolView& pv, bool fp4, const int32_t* keep, const CompactArgs& a, hipStream_t stream) {
+int compact_rows_per_segment(int head_dim, bool fp4) {
+  return head_dim == 128 ? (fp4 ? COMPACT_ROWS<128, true> : COMPACT_ROWS<128, false>) : fp4 ? COMPACT_ROWS<64, true> : COMPACT_ROWS<64, false>;
+}
+
+int launch_compact(const PoolView& pv, bool fp4, const int32_t* keep, uint32_t* marks, size_t n_marks, const CompactArgs& a, hipStream_t stream) {
   if (a.n_req <= 0) return 0;
+  const unsigned chains = 2 * pv.n_kv_heads;
+  const size_t need = compact_marks(a, chains);
+  const bool flagged = a.segments > a.n_req;       // (some chain has several segments)
+  const bool one_by_one = flagged && need > n_marks;
+  if (flagged && !one_by_one) {
+    const int e = launch_fill(marks, 0, need, stream);
+    if (e) return e;
+  }
   return of_pool(pv, fp4, [&](auto dim, auto four, auto direct) {
-    return launch(compact_kernel<dim(), four(), direct()>, dim3((unsigned)a.n_req, 2 * pv.n_kv_heads), 512, stream, pv, keep, a);
+    auto go = [&](auto kernel, int blocks) { return launch(kernel, dim3((unsigned)blocks, chains), COMPACT_THREADS, stream, pv, keep, marks, a); };
+    if (one_by_one) return go(compact_kernel<dim(), four(), direct(), true>, a.n_req);
+    return go(compact_kernel<dim(), four(), direct(), false>, a.segments);
   });
 }
 

@@ -197,3 +197,81 @@ def test_a_captured_copy_and_compaction():
         torch.cuda.synchronize()
         same(c)
     c.close()
+
+
+@pytest.mark.parametrize("dtype,n_kv,dim,lens,share", [
+    (E.ELLM_BF16, 1, 128, [20000, 700, 9000], 0.8), (E.ELLM_BF16, 4, 64, [6000] * 40, 0.5), (E.ELLM_MXFP4, 2, 128, [30000, 40, 2000], 0.9),
+    (E.ELLM_MXFP4, 1, 64, [60000, 5000], 0.3), (E.ELLM_BF16, 8, 128, [3000] * 20, 0.97), (E.ELLM_MXFP4, 8, 128, [1500] * 130, 0.7)])
+def test_compactions_of_many_segments(dtype, n_kv, dim, lens, share):
+    """Rows that move far and near, in chains of many segments whose stores wait for others' reads; three times in a row."""
+    rng = np.random.default_rng(4)
+    total = sum(lens)
+    k, v = (torch.randn(total, n_kv, dim, device="cuda").to(torch.bfloat16) for _ in range(2))
+    row = dim // 2 + dim // 32 if dtype == E.ELLM_MXFP4 else 2 * dim
+    cb = -(-300 * 2 * n_kv * row // 256) * 256
+    T = plain.tokens_per_chunk(cb, n_kv, dim, dtype == E.ELLM_MXFP4)
+    slots = [-(-n // T) for n in lens]
+    buf = torch.zeros(sum(slots), cb, dtype=torch.uint8, device="cuda")
+    pool = E.ellm_pool_create(buf, None, cb, n_kv, n_kv, dim, len(lens), max(slots), dtype=dtype)
+    place, ids = rng.permutation(sum(slots)).astype(np.int32), []
+    for n, s in zip(lens, slots):
+        ids.append(E.ellm_tensor_create(pool, n))
+        E.ellm_tensor_map_chunks(pool, ids[-1], 0, s, place[:s])
+        place = place[s:]
+    E.ellm_kv_append(pool, ids, k, v, lens)
+    want = []
+    for x in (k, v):
+        out = torch.empty_like(x)
+        want.append(out)
+    E.ellm_kv_read(pool, ids, *want)
+    n = list(lens)
+    for turn in range(3):
+        # scattered positions; all but some at the beginning; the last ones
+        keep = [np.sort(rng.permutation(m)[:max(1, int(m * share))]) if turn == 0 else np.arange(min(m - 1, 5 + m // 10), m) if turn == 1 else
+                np.concatenate([np.arange(m // 3), np.arange(m - m // 3, m)]) if m > 3 else np.arange(1) for m in n]
+        at = np.concatenate([b + x for b, x in zip(np.concatenate([[0], np.cumsum(n)[:-1]]), keep)])
+        want = [x[torch.from_numpy(at).cuda()] for x in want]
+        n = [len(x) for x in keep]
+        E.ellm_kv_compact(pool, ids, keep=torch.from_numpy(np.concatenate(keep).astype(np.int32)).cuda(), n_keep=n)
+        got = [torch.empty_like(x) for x in want]
+        E.ellm_kv_read(pool, ids, *got)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    torch.cuda.synchronize()
+    E.ellm_pool_destroy(pool)
+
+
+def test_a_compaction_without_room_for_flags():
+    """Chains of so many segments that the workspace has no room for a flag each go one segment after the other."""
+    n_kv, dim, n = 16, 64, 1100000
+    cb = 1 << 21
+    T = plain.tokens_per_chunk(cb, n_kv, dim, False)
+    slots = -(-n // T)
+    buf = torch.empty(slots, cb, dtype=torch.uint8, device="cuda")
+    pool = E.ellm_pool_create(buf, None, cb, n_kv, n_kv, dim, 1, slots)
+    marks = E.ellm_workspace_bytes(n_kv, n_kv, dim, 1) // 4
+    assert 2 * n_kv * (16 + (n - 1) // 512) > marks
+    t = E.ellm_tensor_create(pool, n)
+    E.ellm_tensor_map_chunks(pool, t, 0, slots)
+    k, v = (torch.randn(n, n_kv, dim, device="cuda", dtype=torch.float16).view(torch.bfloat16) for _ in range(2))
+    E.ellm_kv_append(pool, [t], k, v, [n])
+    keep = torch.arange(1, n, dtype=torch.int32, device="cuda")
+    E.ellm_kv_compact(pool, [t], keep=keep, n_keep=[n - 1])
+    got = [torch.empty_like(k[1:]) for _ in range(2)]
+    E.ellm_kv_read(pool, [t], *got)
+    assert torch.equal(got[0].view(torch.int16), k[1:].view(torch.int16)) and torch.equal(got[1].view(torch.int16), v[1:].view(torch.int16))
+    torch.cuda.synchronize()
+    E.ellm_pool_destroy(pool)
+
+
+def test_decode_after_a_compaction_in_its_workspace():
+    """Both use the workspace of partial results, one behind the other."""
+    c = Cache([5000, 300], 2, 4, 128, 64)
+    q, dq = c.queries()
+    for step in range(3):
+        m = [len(x) for x in c.k]
+        keep = [np.arange(0, x) for x in m]
+        keep[0] = np.delete(keep[0], 7)
+        E.ellm_kv_compact(c.pool, c.ids, keep=torch.from_numpy(np.concatenate(keep).astype(np.int32)).cuda(), n_keep=[len(x) for x in keep])
+        c.k[0], c.v[0] = c.k[0][keep[0]], c.v[0][keep[0]]
+        c.check(c.decode(dq), q)
+    c.close()
