@@ -139,6 +139,8 @@ lib.ellm_debug_decode_kernel.argtypes = [_vp, _i32p, C.c_int32, C.c_int32]
 _calls.bind(np.ndarray, *(C.cast(getattr(lib, n), C.c_void_p).value for n in (
     "ellm_decode_attention", "ellm_decode_attention_noalloc", "ellm_kv_append_decode", "ellm_kv_append", "ellm_kv_premap_next")))
 
+_calls.bind_tokens(*(C.cast(getattr(lib, n), C.c_void_p).value for n in ("ellm_kv_read", "ellm_kv_copy", "ellm_kv_compact")))
+
 EXPORTED = sorted(list(_sigs) + ["ellm_last_error", "ellm_workspace_bytes", "ellm_debug_decode_kernel"])
 
 
@@ -411,6 +413,9 @@ def ellm_kv_append_decode(pool, ids, k_new, v_new, q, out, scale=0.0, stream=Non
 
 
 def ellm_kv_read(pool, ids, k_out, v_out, first=None, n_tokens=None, stream=None, check=True):
+    rc = _calls.read(pool, ids, k_out, v_out, first, n_tokens, stream)
+    if rc is not None:
+        return rc if rc >= 0 else _ret(rc, check)
     keep, p, n = _i32(ids)
     keep_f, pf = _i64(first, n, "first")
     keep_n, pn = _i64(n_tokens, n, "n_tokens")
@@ -418,6 +423,9 @@ def ellm_kv_read(pool, ids, k_out, v_out, first=None, n_tokens=None, stream=None
 
 
 def ellm_kv_copy(pool, src, dst, first=None, n_tokens=None, stream=None, check=True):
+    rc = _calls.copy(pool, src, dst, first, n_tokens, stream)
+    if rc is not None:
+        return rc if rc >= 0 else _ret(rc, check)
     keep, p, n = _i32(src)
     keep_d, pd, _ = _i32(dst)
     _holds(keep_d, n, "dst")
@@ -428,6 +436,9 @@ def ellm_kv_copy(pool, src, dst, first=None, n_tokens=None, stream=None, check=T
 
 def ellm_kv_compact(pool, ids, first=None, keep=None, n_keep=None, flags=0, stream=None, check=True):
     """keep: device tensor of int32 positions. Without n_keep the tensors are cut to first."""
+    rc = _calls.compact(pool, ids, first, keep, n_keep, flags, stream)
+    if rc is not None:
+        return rc if rc >= 0 else _ret(rc, check)
     keep_i, p, n = _i32(ids)
     keep_f, pf = _i64(first, n, "first")
     keep_n, pn = _i64(n_keep, n, "n_keep")

@@ -184,6 +184,84 @@ def test_a_refused_launch_leaves_whole_groups(call):
     E.ellm_pool_destroy(p)
 
 
+class Nothing:
+    """In the place of the native calls: handles no form of these."""
+
+    def __getattr__(self, name):
+        return (lambda *a: None) if name in ("read", "copy", "compact") else getattr(REAL, name)
+
+
+REAL = E.binding._calls
+
+
+def forms(values, dtype):
+    a = np.asarray(values, dtype)
+    wide = np.zeros(2 * len(a), dtype)
+    wide[::2] = a
+    return {"array": a, "list": list(values), "other width": a.astype(np.int32 if dtype == np.int64 else np.int64), "strided": wide[::2],
+            "swapped": a.astype(a.dtype.newbyteorder()), "longer": np.concatenate([a, a])}
+
+
+@pytest.mark.parametrize("ids_form", ["array", "list", "other width", "strided", "swapped"])
+@pytest.mark.parametrize("n_form", ["array", "list", "other width", "strided", "swapped", "longer"])
+def test_native_conversion_and_the_general_one(monkeypatch, ids_form, n_form):
+    """Every form of arguments gives the same results, tables and refusals either way."""
+    import torch
+
+    class Address:
+        def data_ptr(self):
+            return 0x2000
+
+    def walk():
+        p = pool(tensors=4)
+        t = [grown(p, 40, 120), grown(p, 20, 120), grown(p, 0, 120)]
+        ids = lambda *v: forms([t[i] if i < 3 else i for i in v], np.int32)[ids_form]  # noqa: E731
+        n = lambda *v: forms(v, np.int64)[n_form]  # noqa: E731
+        seen = []
+
+        def call(f, *a, **k):
+            try:
+                seen.append(f(p, *a, stream=0, **k))
+            except Exception as e:
+                seen.append((type(e).__name__, getattr(e, "code", None)))
+
+        for at in (0x1000, None, Address(), torch.zeros(4)):
+            call(E.ellm_kv_read, ids(0, 1), at, 0x3000, first=n(1, 20), n_tokens=n(2, 0))
+            call(E.ellm_kv_read, ids(2), 0x3000, at)
+        call(E.ellm_kv_read, ids(9), 16, 16, check=False)
+        call(E.ellm_kv_copy, ids(0, 1), ids(2), first=n(1, 2))
+        call(E.ellm_kv_copy, ids(0), ids(2))
+        call(E.ellm_kv_copy, ids(0), ids(1, 2), first=n(7), n_tokens=n(3))
+        call(E.ellm_kv_copy, ids(0), ids(0), check=False)
+        for keep in (0x1000, Address(), torch.zeros(4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int64),
+                     torch.zeros(8, dtype=torch.int32)[::2], None, "x"):
+            call(E.ellm_kv_compact, ids(0, 1), first=n(1, 2), keep=keep, n_keep=n(3, 1))
+        for flags in (0, 1, 2, True):
+            call(E.ellm_kv_compact, ids(0, 1), first=n(2, 1), flags=flags, check=False)
+        call(E.ellm_kv_compact, ids(0, 1), first=n(1))
+        call(E.ellm_kv_compact, ids(0, 1))
+        after = state(p, 3)
+        E.ellm_pool_destroy(p)
+        return seen, after
+
+    native = walk()
+    assert native[0].count(0) >= 5
+    monkeypatch.setattr(E.binding, "_calls", Nothing())
+    assert walk() == native
+
+
+def test_plain_arguments_are_converted_natively():
+    p = pool()
+    a, b = grown(p, 9, 40), grown(p, 0, 40)
+    ids, other, one = np.array([a], np.int32), np.array([b], np.int32), np.array([1], np.int64)
+    assert REAL.read(p, ids, 16, 16, None, one, 0) == ERR.NO_DEVICE
+    assert REAL.copy(p, ids, other, one, None, 0) == 0 and REAL.compact(p, ids, one, 16, one, 0, 0) == 0
+    assert (length(p, a), length(p, b)) == (2, 8)
+    with pytest.raises(TypeError):
+        REAL.copy(p, ids)
+    E.ellm_pool_destroy(p)
+
+
 # ---- the format that GPU tests compare with ---------------------------------------------------------
 def test_plain_format():
     one = lambda *x: np.array(list(x) + [0.0] * (32 - len(x)))  # noqa: E731
