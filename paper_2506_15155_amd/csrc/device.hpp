@@ -175,7 +175,7 @@ __device__ __forceinline__ const char* chunk_addr(const PoolView& pv, const Tens
 // s_waitcnt immediates (gfx9 encoding): vmcnt in bits 3:0 and 15:14, expcnt 6:4, lgkmcnt 11:8
 constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0F70; }
 
-constexpr float NEG_BIG = -1.0e30f;   // finite stand-in for "no score yet"; exp2(NEG_BIG - x) == 0
+constexpr float NEG_BIG = -3.402823466e38f;   // finite stand-in for "no score yet", below every score; exp2(NEG_BIG - x) == 0 but for x near it
 
 // 16x16x32 matrix products; what becomes of a weight that is multiplied as two bf16 values
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;

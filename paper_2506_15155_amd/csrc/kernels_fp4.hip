@@ -53,6 +53,11 @@ __device__ __forceinline__ int32_t stage_read(int32_t row, int32_t piece, int32_
 // request, and the values are exact down to 2^-36 of it. (Weights as sums of two bf16 values, which need no such care, take twice as
 // many products and 60 more of 310 instructions a tile: 16 requests of 32768 to 131072 tokens, 8 q heads each 249 us a call.)
 constexpr int WEIGHT_BITS = 12, VALUE_BITS = 13;
+// Scores over LARGE_SCORE are multiples of 2^-3 and more: the product with the scale is then rounded before the maximum is taken
+// off, so that the largest comes out as 0 and no weight outside the range, and WEIGHT_BITS, which might be rounded up, stays away.
+constexpr float LARGE_SCORE = 0x1p20f;
+// what weights are relative to, for a largest score of `top`
+__device__ __forceinline__ float reference(float top) { return __builtin_fabsf(top) > LARGE_SCORE ? top : top - WEIGHT_BITS; }
 
 typedef short __attribute__((ext_vector_type(4))) s16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
@@ -84,7 +89,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   const uint64_t head_rows = (uint64_t)(2 * g) * plane, head_scales = fp4_scales_at<D>(pv) + (uint64_t)(2 * g) * scale_plane;
 
   // Scores are kept without the scale, of which only the sign goes into the query (the maximum has to be one): its size is part
-  // of the exponential's argument, in log2 units, as are the maximum m and the other kernels' partial results.
+  // of the exponential's argument, in log2 units, as are the reference m of the maximum and the other kernels' partial results.
   const float size = __builtin_fabsf(scale_log2);
   const uint32_t sign = scale_log2 < 0.f ? 0x80008000u : 0u;
 
@@ -267,7 +272,8 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   };
 
   // ---- arithmetic ----
-  float m = NEG_BIG, l = 0.f;
+  float top = NEG_BIG, m = NEG_BIG, l = 0.f;         // the maximum so far, what weights are relative to, their sum
+  bool large = false;                                // (of some head)
   uint32_t largest = 0;                              // of V's scales in the request so far
   f32x4_t acc[NB], s[U];
   auto scores = [&](const Tile& t) __attribute__((always_inline)) {
@@ -301,8 +307,9 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   };
   auto weigh = [&](const Tile& t, char* stage) __attribute__((always_inline)) {
     if (t.flags & T_FIRST) {
-      m = NEG_BIG;
+      top = m = NEG_BIG;
       l = 0.f;
+      large = false;
 #pragma unroll
       for (int n = 0; n < NB; n++) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
@@ -334,34 +341,41 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
     for (int u = 1; u < U; u++) mx = fmaxf(mx, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
-    const float mn = fmaxf(m, max_xor32(max_xor16(mx)) * size);
-    if (__builtin_amdgcn_ballot_w64(mn > m)) {       // some head has a new maximum
-      const float alpha = fast_exp2(m - mn);
+    const float tn = fmaxf(top, max_xor32(max_xor16(mx)) * size);
+    if (__builtin_amdgcn_ballot_w64(tn > top)) {     // some head has a new maximum
+      const float mn = reference(tn), alpha = fast_exp2(m - mn);
       l *= alpha;
 #pragma unroll
       for (int n = 0; n < NB; n++) acc[n] *= alpha;
+      top = tn;
       m = mn;
+      large = __builtin_amdgcn_ballot_w64(__builtin_fabsf(top) > LARGE_SCORE) != 0;
     }
     // the largest of V's scales in this tile (a block that is NaN has none)
-    uint32_t top = 0;
+    uint32_t scale_top = 0;
 #pragma unroll
-    for (int u = 0; u < U; u++) top = max(top, vs[u] == FP4_SCALE_NAN ? 0u : vs[u]);
-    if ((t.flags & T_FIRST) || __builtin_amdgcn_ballot_w64(top > largest)) {
-      const uint32_t now = wave_max_u32(top), before = t.flags & T_FIRST ? now : largest;
+    for (int u = 0; u < U; u++) scale_top = max(scale_top, vs[u] == FP4_SCALE_NAN ? 0u : vs[u]);
+    if ((t.flags & T_FIRST) || __builtin_amdgcn_ballot_w64(scale_top > largest)) {
+      const uint32_t now = wave_max_u32(scale_top), before = t.flags & T_FIRST ? now : largest;
       largest = max(now, before);
 #pragma unroll
       for (int n = 0; n < NB; n++)
 #pragma unroll
         for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], (int)(before - largest));
     }
-    const float below = WEIGHT_BITS - m;
+    float times = size;
+    if (large) {
+#pragma unroll
+      for (int u = 0; u < U; u++) s[u] *= size;
+      times = 1.f;
+    }
 #pragma unroll
     for (int u = 0; u < U; u += 2) {
       words4_t weights;
 #pragma unroll
       for (int h = 0; h < 4; h++) {
         const f32x4_t& x = s[u + h / 2];
-        const float p0 = fast_exp2(x[2 * (h & 1)] * size + below), p1 = fast_exp2(x[2 * (h & 1) + 1] * size + below);
+        const float p0 = fast_exp2(x[2 * (h & 1)] * times - m), p1 = fast_exp2(x[2 * (h & 1) + 1] * times - m);
         l += p0 + p1;
         weights[h] = pack_f16(p0, p1);
       }
@@ -397,7 +411,6 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     for (int n = 0; n < NB; n++)
 #pragma unroll
       for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], (int)largest - (127 + VALUE_BITS));
-    m -= WEIGHT_BITS;                                // (what the weights are relative to)
   };
   // which piece of a row, in the order of partial_dim() for units, has dims 16 n + 4 g16 .. + 3
   auto piece = [&](int n) __attribute__((always_inline)) {
@@ -533,7 +546,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
 }
 
 template <int D, int U, int HEADS, int SW, bool RUN, bool APPEND, bool DIRECT, class Args>
-__global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(2, 2))) void decode_fp4_kernel(
+__global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(D * HEADS > 1024 ? 1 : 2, D * HEADS > 1024 ? 1 : 2))) void decode_fp4_kernel(
     PoolView pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new, const char* __restrict__ v_new,
     float* __restrict__ ws, uint16_t* __restrict__ out, float scale_log2, int32_t g_first, int32_t n_heads, Args a) {
   in_launch(pv, ws, a, [&](const PoolView& pv, float* ws, const auto& a, int32_t workgroup) __attribute__((always_inline)) {

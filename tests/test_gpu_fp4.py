@@ -274,6 +274,36 @@ def test_scale_and_large_scores():
     c.close()
 
 
+@pytest.mark.parametrize("n_kv,group,dim,tokens,lens", [(2, 4, 128, 64, [333, 17]), (1, 16, 64, 24, [333, 70]), (8, 4, 128, 512, [3000] * 5)])
+def test_scores_of_any_size(n_kv, group, dim, tokens, lens):
+    """Scores that differ by far more than 2^24: the result is the V row of the largest one. Scores that are all alike: the mean
+    of V, of however large scores."""
+    c = Cache(lens, n_kv, group, dim, tokens, room=40)
+    q, dq = c.queries()
+    for exponent in (16, 20, 23, 24, 26, 27, 30, 33, 60, 100):
+        for sign in (1, -1):
+            scale = sign * 1.37 * 2.0 ** exponent
+            got = plain.values(host(c.decode(dq, scale=scale)))
+            for i in range(len(lens)):
+                for h in range(n_kv * group):
+                    k, v = c.k[i][:, h // group], c.v[i][:, h // group]
+                    s = k @ q[i, h] * sign
+                    # (a score of 128 products in 32 bits is 2^-17 of the sum of their magnitudes off, which is under 1000; 0.02 * 2^16 is far
+                    # more than any exponential needs)
+                    near = v[s >= s.max() - 0.02]
+                    tol = TOL * np.abs(v).max()
+                    assert ((got[i, h] >= near.min(0) - tol) & (got[i, h] <= near.max(0) + tol)).all(), (scale, i, h)
+    c.close()
+    c = Cache([0] * len(lens), n_kv, group, dim, tokens, room=max(lens))
+    k, v = c.draw(sum(lens))
+    k[:] = k[0]
+    c.append(k, v, lens)
+    for exponent in (16, 20, 23, 24, 26, 27, 30, 33, 60, 100):
+        for sign in (1, -1):
+            c.check(c.decode(dq, scale=sign * 1.37 * 2.0 ** exponent), q, scale=0)
+    c.close()
+
+
 def test_remapped_chunks_and_host_round_trips_keep_the_bits():
     lens = [100, 500, 33]
     a, b = Cache(lens, 2, 4, 128, 48, seed=1, host_chunks=16), Cache(lens, 2, 4, 128, 48, seed=1)
