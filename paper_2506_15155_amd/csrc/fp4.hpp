@@ -64,16 +64,15 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 __device__ __forceinline__ f32x4_t mfma16_f16(words4_t a, words4_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
 }
-// the largest of all lanes' values, in every lane
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, DPP_QUAD_XOR1, 0xf, 0xf, false));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, DPP_QUAD_XOR2, 0xf, 0xf, false));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, DPP_ROW_HALF_MIRROR, 0xf, 0xf, false));
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, DPP_ROW_MIRROR, 0xf, 0xf, false));
+// the largest value of all lanes with the same lane & 3, in each of them
+__device__ __forceinline__ uint32_t max_of_quarter(uint32_t v) {
+  constexpr int ROW_ROR4 = 0x124, ROW_ROR8 = 0x128;
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ROW_ROR4, 0xf, 0xf, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ROW_ROR8, 0xf, 0xf, false));
   const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
   v = max(a[0], a[1]);
   const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return (uint32_t)__builtin_amdgcn_readfirstlane((int)max(b[0], b[1]));
+  return max(b[0], b[1]);
 }
 
 // the larger of the value and that of lane ^ 1, of lane ^ 2

@@ -49,8 +49,8 @@ __device__ __forceinline__ int32_t stage_read(int32_t row, int32_t piece, int32_
 
 // The second product is one of fp16 values, of more bits than bf16 and a smaller range, which is used to its ends. A weight is held
 // relative to the running maximum, at most 2^WEIGHT_BITS; what its rounding loses is 2^-12 of it, or, of the smallest ones, 2^-25 of
-// 1 / 2^WEIGHT_BITS: 2^-37 of the largest weight. A scale of V is held relative to the largest one that the wave has met in the
-// request, and the values are exact down to 2^-36 of it. (Weights as sums of two bf16 values, which need no such care, take twice as
+// 1 / 2^WEIGHT_BITS: 2^-37 of the largest weight. A scale of V is held relative to the largest one of the same block that the
+// wave has met in the request, and the values are exact down to 2^-36 of it. (Weights as sums of two bf16 values, which need no such care, take twice as
 // many products and 60 more of 310 instructions a tile: 16 requests of 32768 to 131072 tokens, 8 q heads each 249 us a call.)
 constexpr int WEIGHT_BITS = 12, VALUE_BITS = 13;
 // Scores over LARGE_SCORE are multiples of 2^-3 and more: the product with the scale is then rounded before the maximum is taken
@@ -274,7 +274,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   // ---- arithmetic ----
   float top = NEG_BIG, m = NEG_BIG, l = 0.f;         // the maximum so far, what weights are relative to, their sum
   bool large = false;                                // (of some head)
-  uint32_t largest = 0;                              // of V's scales in the request so far
+  uint32_t largest = 0;                              // of V's scales in the request so far, of the block that lane & 3 is a quarter of
   f32x4_t acc[NB], s[U];
   auto scores = [&](const Tile& t) __attribute__((always_inline)) {
     if (APPEND && (t.flags & T_LAST)) {
@@ -356,12 +356,13 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
 #pragma unroll
     for (int u = 0; u < U; u++) scale_top = max(scale_top, vs[u] == FP4_SCALE_NAN ? 0u : vs[u]);
     if ((t.flags & T_FIRST) || __builtin_amdgcn_ballot_w64(scale_top > largest)) {
-      const uint32_t now = wave_max_u32(scale_top), before = t.flags & T_FIRST ? now : largest;
+      const uint32_t now = max_of_quarter(scale_top), before = t.flags & T_FIRST ? now : largest;
       largest = max(now, before);
+      const int by = (int)(before - largest);
 #pragma unroll
       for (int n = 0; n < NB; n++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], (int)(before - largest));
+        for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], __builtin_amdgcn_readlane(by, n / (W / 2)));
     }
     float times = size;
     if (large) {
@@ -410,7 +411,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
 #pragma unroll
     for (int n = 0; n < NB; n++)
 #pragma unroll
-      for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], (int)largest - (127 + VALUE_BITS));
+      for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], __builtin_amdgcn_readlane((int)largest - (127 + VALUE_BITS), n / (W / 2)));
   };
   // which piece of a row, in the order of partial_dim() for units, has dims 16 n + 4 g16 .. + 3
   auto piece = [&](int n) __attribute__((always_inline)) {

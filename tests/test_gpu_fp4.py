@@ -304,6 +304,22 @@ def test_scores_of_any_size(n_kv, group, dim, tokens, lens):
     c.close()
 
 
+@pytest.mark.parametrize("n_kv,group,dim,tokens,lens", [(2, 4, 128, 64, [333, 17, 1]), (1, 16, 64, 24, [333, 70]), (8, 4, 128, 512, [3000] * 5), (1, 20, 128, 16, [100])])
+def test_blocks_of_very_different_magnitudes(n_kv, group, dim, tokens, lens):
+    """Each block of 32 dims of V has its result to the same part of its own largest value, whatever the others' are."""
+    c = Cache([0] * len(lens), n_kv, group, dim, tokens, room=max(lens))
+    k, v = c.draw(sum(lens))
+    v *= np.repeat(2.0 ** c.rng.permutation([-90, 70, 0, -25])[:dim // 32], 32)
+    c.append(k, plain.bf16(v), lens)
+    q, dq = c.queries()
+    got = plain.values(host(c.decode(dq)))
+    for i in range(len(lens)):
+        want = plain.attention(q[i], c.k[i], c.v[i])
+        top = np.repeat(np.abs(c.v[i]).reshape(-1, n_kv, dim // 32, 32).max((0, 3)), group, 0)
+        assert (np.abs(got[i] - want) <= TOL * np.repeat(top, 32, -1)).all(), i
+    c.close()
+
+
 def test_remapped_chunks_and_host_round_trips_keep_the_bits():
     lens = [100, 500, 33]
     a, b = Cache(lens, 2, 4, 128, 48, seed=1, host_chunks=16), Cache(lens, 2, 4, 128, 48, seed=1)
