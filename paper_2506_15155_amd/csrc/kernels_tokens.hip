@@ -42,14 +42,13 @@ struct Tensor {
   }
 };
 
-// the last i with first[i] <= x
+// the last i < n with first[i] <= x, in one round of loads: a search by halves, whose loads wait for each other, cost the appending of
+// a token for 64 requests and its reading back 0.8 us each (3.9 -> 3.1)
 __device__ __forceinline__ int32_t find_last(const int32_t* first, int32_t n, int32_t x) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= x) lo = mid; else hi = mid - 1;
-  }
-  return lo;
+  const int lane = threadIdx.x & 63;
+  static_assert(MAX_LAUNCH_REQ == 128, "two entries a lane");
+  const int32_t f0 = first[lane], f1 = first[64 + lane];
+  return __popcll(__builtin_amdgcn_ballot_w64(lane < n && f0 <= x)) + __popcll(__builtin_amdgcn_ballot_w64(64 + lane < n && f1 <= x)) - 1;
 }
 
 // A workgroup's tokens of the dense side: request b, positions p0 .. p1 - 1
@@ -134,8 +133,14 @@ __global__ __launch_bounds__(256) void read_tokens_kernel(PoolView pv, char* __r
 }
 
 // ---------------------------------------------------------------------------------------------
-// Copying: a group's rows are read once and go to all of its destinations.
+// Copying: a group's rows are read once and go to all of its destinations, one after the other. A few workgroups would take long
+// over many destinations (each waits for the table): up to COPY_WORKGROUPS in all, the destinations are split among several, which
+// read the same rows. us of the kernel: 260 tokens of 4-bit rows, 8 kv heads of 128, to 8 tensors (24 workgroups) 10.2, two parts 6.9, four
+// 5.5, eight 4.8; four of 2000 to 8192 bf16 tokens to 4 tensors each (2500) 100, 110 in two parts.
+// Rows are read without a streaming hint: they are the source's, which is read again. That call, sources in the last-level cache
+// 99 us with the hint and 80 without, otherwise 100 and 95 (5.3 TB/s); stores without it 103, blocks of 32 KB 99.
 // ---------------------------------------------------------------------------------------------
+constexpr int COPY_WORKGROUPS = 1024;
 template <int D, bool FP4> constexpr int COPY_TOKENS = COPY_BYTES / (2 * Rows<D, FP4>::BYTES);
 
 template <int D, bool FP4, bool DIRECT>
@@ -152,7 +157,7 @@ __global__ __launch_bounds__(256) void copy_tokens_kernel(PoolView pv, CopyToken
   for (int i = 0; i < N; i++) {
     if (token_of(i) >= rows) continue;
     const RowAt at = from.row(pv, a.first[g] + k0 + token_of(i));
-    x[i] = load_stream16(at.chunk + R::rows_at(pv, h, plane_of(i)) + at.row * R::BYTES + sub * 16);
+    x[i] = *reinterpret_cast<const uint4*>(at.chunk + R::rows_at(pv, h, plane_of(i)) + at.row * R::BYTES + sub * 16);
   }
   // the scales of a row by one lane: TOKENS rows of either plane are 256 lanes (heads of 64: two rounds)
   constexpr int NS = FP4 ? 2 * TOKENS / 256 : 1;
@@ -167,7 +172,7 @@ __global__ __launch_bounds__(256) void copy_tokens_kernel(PoolView pv, CopyToken
       scales[i] = *reinterpret_cast<const scales_t*>(at.chunk + R::scales_at(pv, h, r / TOKENS) + at.row * R::SCALES);
     }
   }
-  for (int32_t d = a.dst0[g]; d < a.dst0[g + 1]; d++) {
+  for (int32_t d = a.dst0[g] + (int32_t)blockIdx.z; d < a.dst0[g + 1]; d += (int32_t)gridDim.z) {
     const Tensor<DIRECT> to(pv, a.dst[d]);
     const int32_t pos = a.pos[d] + k0;
 #pragma unroll
@@ -311,8 +316,11 @@ int copy_tokens_per_block(int head_dim, bool fp4) {
 
 int launch_copy_tokens(const PoolView& pv, bool fp4, const CopyTokenArgs& a, hipStream_t stream) {
   if (a.blocks <= 0) return 0;
+  int32_t most = 1;
+  for (int32_t g = 0; g < a.n_groups; g++) most = std::max(most, a.dst0[g + 1] - a.dst0[g]);
+  const int32_t parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, COPY_WORKGROUPS / ((int64_t)a.blocks * pv.n_kv_heads)));
   return of_pool(pv, fp4, [&](auto dim, auto four, auto direct) {
-    return launch(copy_tokens_kernel<dim(), four(), direct()>, dim3((unsigned)a.blocks, pv.n_kv_heads), 256, stream, pv, a);
+    return launch(copy_tokens_kernel<dim(), four(), direct()>, dim3((unsigned)a.blocks, pv.n_kv_heads, parts), 256, stream, pv, a);
   });
 }
 
