@@ -345,7 +345,9 @@ int ellm_kv_copy(ellm_pool* pool, const ellm_tensor_id* src, const ellm_tensor_i
  *   Without n_keep (or with zeros) lengths are cut to first[b], and nothing is launched.
  *   flags: ELLM_COMPACT_UNMAP: slots that hold no token afterwards are emptied, as by ellm_tensor_unmap_chunks.
  *   keep is read by the launch. Positions that break the rules above make the rows behind first[b] undefined, and touch nothing else.
- *   Enqueued on `stream`; returns without waiting.
+ *   Enqueued on `stream`; returns without waiting. Large moves keep flags in the pool's workspace of partial results: calls are put in
+ *   order, but replays of graphs that hold this call must not overlap another replay or call of it, ellm_decode_attention or
+ *   ellm_kv_append_decode on the same pool.
  * Checks: unknown flag, batch < 0 -> INVALID; per request in order: bad or repeated handle, negative position or count -> INVALID;
  * first > len, n_keep > len - first -> RANGE; with n_keep > 0 the slots of first .. len - 1 ascending: empty -> UNMAPPED, on host ->
  * NOT_RESIDENT. NULL keep with tokens to keep -> INVALID; more than 2^30 / n_kv_heads of them -> RANGE. Works in one launch per 128
@@ -358,7 +360,8 @@ int ellm_kv_compact(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, c
  *   For q head h, kv head g = h / G:  s_t = scale * <q_h, K_t,g>,  w = softmax_t(s),
  *   out_h = sum_t w_t * V_t,g  for t = 0 .. len-1, no mask. scale = 0 selects 1/sqrt(head_dim).
  *   fp32 accumulation (softmax weights are rounded to bf16 before they multiply V and before they
- *   are summed, or, in some kernels, multiply V as two bf16 values), output rounded to nearest-even bf16. Split over the sequence with a partition
+ *   are summed, or, in some kernels, multiply V as two bf16 values; ELLM_MXFP4: weights multiply V as fp16 values, to 2^-12 of each
+ *   or 2^-37 of the largest, and V counts down to 2^-36 of the largest scale that the request has in the same 32 dims), output rounded to nearest-even bf16. Split over the sequence with a partition
  *   that depends only on the lengths in the batch, the pool geometry and the device's wave
  *   capacity, never on physical chunk ids, so results are bitwise reproducible and invariant
  *   under remapping.

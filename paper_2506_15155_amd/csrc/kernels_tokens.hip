@@ -211,6 +211,8 @@ __global__ __launch_bounds__(256) void copy_tokens_kernel(PoolView pv, CopyToken
 // ---------------------------------------------------------------------------------------------
 template <int D, bool FP4> constexpr int COMPACT_ROWS = COMPACT_BYTES / Rows<D, FP4>::BYTES;
 constexpr int COMPACT_THREADS = 1024;
+// A wait takes microseconds. It ends all the same (after some seconds) where something else has written over the flags, which calls in order do not.
+constexpr int32_t MOST_TURNS = 1 << 22;
 
 template <int D, bool FP4, bool DIRECT, bool ONE_BY_ONE>
 __global__ __launch_bounds__(COMPACT_THREADS) void compact_kernel(PoolView pv, const int32_t* __restrict__ keep, uint32_t* __restrict__ marks, CompactArgs a) {
@@ -260,7 +262,8 @@ __global__ __launch_bounds__(COMPACT_THREADS) void compact_kernel(PoolView pv, c
       // the segments before this one that read as far as this one stores
       for (int32_t j = threadIdx.x; j < seg; j += COMPACT_THREADS)
         if (source((j + 1) * STEP - 1) >= first + i0)
-          while (!__hip_atomic_load(flags + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) __builtin_amdgcn_s_sleep(1);
+          for (int32_t turn = 0; turn < MOST_TURNS && !__hip_atomic_load(flags + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); turn++)
+            __builtin_amdgcn_s_sleep(1);
       __syncthreads();
     }
 #pragma unroll
