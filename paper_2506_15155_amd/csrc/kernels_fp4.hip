@@ -273,7 +273,8 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
 
   // ---- arithmetic ----
   float top = NEG_BIG, m = NEG_BIG, l = 0.f;         // the maximum so far, what weights are relative to, their sum
-  bool large = false;                                // (of some head)
+  float times = size;                                // what scores still have to be multiplied by: 1 if some head's maximum is large
+  bool large = false;
   uint32_t largest = 0;                              // of V's scales in the request so far, of the block that lane & 3 is a quarter of
   f32x4_t acc[NB], s[U];
   auto scores = [&](const Tile& t) __attribute__((always_inline)) {
@@ -310,6 +311,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       top = m = NEG_BIG;
       l = 0.f;
       large = false;
+      times = size;
 #pragma unroll
       for (int n = 0; n < NB; n++) acc[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
@@ -342,7 +344,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
 #pragma unroll
     for (int u = 1; u < U; u++) mx = fmaxf(mx, fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])));
     const float tn = fmaxf(top, max_xor32(max_xor16(mx)) * size);
-    if (__builtin_amdgcn_ballot_w64(tn > top)) {     // some head has a new maximum
+    if (__builtin_amdgcn_ballot_w64(tn > top) != 0 || large) {     // some head has a new maximum, or a large one
       const float mn = reference(tn), alpha = fast_exp2(m - mn);
       l *= alpha;
 #pragma unroll
@@ -350,6 +352,10 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       top = tn;
       m = mn;
       large = __builtin_amdgcn_ballot_w64(__builtin_fabsf(top) > LARGE_SCORE) != 0;
+      times = large ? 1.f : size;
+      if (large)
+#pragma unroll
+        for (int u = 0; u < U; u++) s[u] *= size;
     }
     // the largest of V's scales in this tile (a block that is NaN has none)
     uint32_t scale_top = 0;
@@ -363,12 +369,6 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       for (int n = 0; n < NB; n++)
 #pragma unroll
         for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], __builtin_amdgcn_readlane(by, n / (W / 2)));
-    }
-    float times = size;
-    if (large) {
-#pragma unroll
-      for (int u = 0; u < U; u++) s[u] *= size;
-      times = 1.f;
     }
 #pragma unroll
     for (int u = 0; u < U; u += 2) {
