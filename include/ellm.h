@@ -303,7 +303,7 @@ int ellm_pool_set_act_busy(ellm_pool* pool, const int32_t* chunk_ids, int32_t n,
  *   k_new, v_new (device): [sum(n_new)][n_kv_heads][head_dim] bf16, request b's tokens start at row
  *   sum(n_new[0..b)). Token i of request b is written at position len_b + i; afterwards
  *   len_b += n_new[b]. Enqueued on `stream` (a hipStream_t); returns without waiting.
- *   An ELLM_MXFP4 pool quantises the rows as it writes them.
+ *   An ELLM_MXFP4 pool quantises the rows as it writes them; its tensors hold less than 2^31 tokens (RANGE).
  * Checks: batch < 0 -> INVALID; per request in order: bad or repeated handle, n_new < 0 -> INVALID;
  * len + n_new > max_tokens -> RANGE; slots covering the new tokens in ascending order: empty ->
  * UNMAPPED, on host -> NOT_RESIDENT. NULL k_new / v_new with tokens to write -> INVALID.
@@ -321,7 +321,8 @@ int ellm_kv_append(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, co
  *   without waiting.
  * Checks: batch < 0 -> INVALID; per request in order: bad handle, negative position or count -> INVALID; tokens past the
  * length -> RANGE; their slots ascending: empty -> UNMAPPED, on host -> NOT_RESIDENT. NULL k_out / v_out with tokens to read ->
- * INVALID; more than 2^30 / n_kv_heads tokens -> RANGE. Works in one launch per 128 requests, like ellm_kv_append. */
+ * INVALID; 2^30 / n_kv_heads tokens or more, or tensors and these together of 2^31 -> RANGE (in the two calls below too). Works in one
+ * launch per 128 requests, like ellm_kv_append. */
 int ellm_kv_read(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, const int64_t* first, const int64_t* n_tokens,
                  void* k_out, void* v_out, void* stream);
 
@@ -334,7 +335,7 @@ int ellm_kv_read(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, cons
  *   at a time). Enqueued on `stream`; returns without waiting.
  * Checks: n < 0 -> INVALID; every dst in order: bad or repeated handle -> INVALID; per pair in order: src as in ellm_kv_read, also a
  * destination -> INVALID, dst: len + n_tokens > max_tokens -> RANGE, slots of the new tokens ascending: empty -> UNMAPPED, on
- * host -> NOT_RESIDENT. More than 2^30 / n_kv_heads tokens -> RANGE. Works in one launch per 128 pairs, like ellm_kv_append. */
+ * host -> NOT_RESIDENT. 2^30 / n_kv_heads tokens or more -> RANGE. Works in one launch per 128 pairs, like ellm_kv_append. */
 int ellm_kv_copy(ellm_pool* pool, const ellm_tensor_id* src, const ellm_tensor_id* dst, int32_t n, const int64_t* first,
                  const int64_t* n_tokens, void* stream);
 
@@ -350,7 +351,7 @@ int ellm_kv_copy(ellm_pool* pool, const ellm_tensor_id* src, const ellm_tensor_i
  *   ellm_kv_append_decode on the same pool.
  * Checks: unknown flag, batch < 0 -> INVALID; per request in order: bad or repeated handle, negative position or count -> INVALID;
  * first > len, n_keep > len - first -> RANGE; with n_keep > 0 the slots of first .. len - 1 ascending: empty -> UNMAPPED, on host ->
- * NOT_RESIDENT. NULL keep with tokens to keep -> INVALID; more than 2^30 / n_kv_heads of them -> RANGE. Works in one launch per 128
+ * NOT_RESIDENT. NULL keep with tokens to keep -> INVALID; 2^30 / n_kv_heads of them or more -> RANGE. Works in one launch per 128
  * requests; lengths and slots of a group change when its launch has been accepted, as in ellm_kv_append. */
 int ellm_kv_compact(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, const int64_t* first, const int32_t* keep,
                     const int64_t* n_keep, uint32_t flags, void* stream);

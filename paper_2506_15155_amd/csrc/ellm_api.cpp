@@ -1101,9 +1101,10 @@ bool launch_refused(ellm_pool* p) { return p->fail_launch_in > 0 && --p->fail_la
 // ---- calls over tokens: quantised append, reading, copying, compacting ----
 // the kernels number tokens, and rows of a call's dense side, in 32 bits
 int fits_one_call(ellm_pool* p, int64_t total, const ellm_tensor_id* ids, int32_t n, const char* call) {
+  if (total == 0) return ELLM_OK;
   bool fits = total <= 0x7fffffffll / (2 * p->geom.n_kv_heads);
   for (int32_t i = 0; i < n && fits; i++) fits = p->core->tensor(ids[i])->len + total <= 0x7fffffffll;
-  return fits ? ELLM_OK : set_err(ELLM_ERR_RANGE, std::string(call) + ": too many tokens in one call");
+  return fits ? ELLM_OK : set_err(ELLM_ERR_RANGE, std::string(call) + ": too many tokens in one call, or in a tensor");
 }
 
 // Requests b0 .. b0 + nb - 1 of p->n_eff tokens each, at the ends of their tensors (first NULL) or from first[b] on. Returns
@@ -1307,6 +1308,7 @@ int ellm_kv_append(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, const
   if (rc) return rc;
   if (total > 0 && (!k_new || !v_new)) return set_err(ELLM_ERR_INVALID, "kv_append: NULL k_new / v_new");
   if (total > 0x7fffffffll / (2 * p->geom.n_kv_heads)) return set_err(ELLM_ERR_RANGE, "kv_append: too many tokens in one call");
+  if (p->geom.fp4 && (rc = fits_one_call(p, total, ids, batch, "kv_append"))) return rc;
   if (total == 0) return ELLM_OK;
   hipStream_t stream = (hipStream_t)stream_;
   int32_t most_new = 0;

@@ -144,6 +144,29 @@ def test_refusals_change_nothing():
     E.ellm_pool_destroy(p)
 
 
+def test_tensors_of_2_to_the_31_tokens():
+    """The kernels number positions in 32 bits: what would pass them is refused; lengths can be cut all the same."""
+    most = 3 << 30
+    for dtype in (E.ELLM_BF16, E.ELLM_MXFP4):
+        cb = 1 << 31
+        p = E.ellm_pool_create(None, None, cb, 1, 1, 64, 3, 400, flags=1, device_bytes=800 * cb, dtype=dtype)
+        T = E.ellm_pool_get_geometry(p)["tokens_per_chunk"]
+        t = E.ellm_tensor_create(p, most)
+        E.ellm_tensor_map_chunks(p, t, 0, -(-most // T))
+        small = E.ellm_tensor_create(p, 100)
+        E.ellm_tensor_map_chunks(p, small, 0, 1)
+        add = lambda n: E.ellm_kv_append(p, [t], 16, 16, [n], check=False)  # noqa: E731
+        assert add(1 << 30) == ERR.RANGE
+        assert add((1 << 30) - 1) == add((1 << 30) - 1) == add(1) == 0 and length(p, t) == (1 << 31) - 1
+        assert add(1) == (ERR.RANGE if dtype == E.ELLM_MXFP4 else 0)
+        assert E.ellm_kv_read(p, [t], 16, 16, first=[5], n_tokens=[1], check=False) == ERR.RANGE
+        assert E.ellm_kv_copy(p, [t], [small], first=[5], n_tokens=[1], check=False) == ERR.RANGE
+        assert E.ellm_kv_compact(p, [t], keep=16, n_keep=[1], check=False) == ERR.RANGE
+        assert E.ellm_kv_compact(p, [t], first=[(1 << 31) - 1], check=False) == E.ellm_kv_compact(p, [t], first=[7], check=False) == 0
+        assert length(p, t) == 7 and E.ellm_kv_copy(p, [t], [small], check=False) == 0 and length(p, small) == 7
+        E.ellm_pool_destroy(p)
+
+
 def test_binding_refuses_short_arrays():
     import torch
     p = pool()
