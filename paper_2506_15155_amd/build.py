@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libellm.so")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 CALLS_SOURCE = os.path.join(CSRC, "python_calls.cpp")
 SOURCES = ["pool_core.cpp", "ellm_api.cpp", "kernels.hip", "kernels_fp4.hip", "kernels_tokens.hip"]
-HEADERS = ["pool_core.hpp", "kernels.hpp", "device.hpp", "fp4.hpp", "divide.hpp", "map_queue.hpp", os.path.join(ROOT, "include", "ellm.h")]
+HEADERS = ["pool_core.hpp", "kernels.hpp", "device.hpp", "fp4.hpp", "fp4_walk.hpp", "divide.hpp", "map_queue.hpp", os.path.join(ROOT, "include", "ellm.h")]
 
 # packed-fp32 instructions are switched off for all device code of this library
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

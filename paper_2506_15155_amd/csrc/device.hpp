@@ -194,12 +194,6 @@ __device__ __forceinline__ uint32_t bf16_below(float p) {
 // ---------------------------------------------------------------------------------------------
 // work partition shared by the partial pass, the combine pass and the calibration kernel
 // ---------------------------------------------------------------------------------------------
-// number of units (tiles) of a sequence of len tokens (neither straddles a chunk)
-__device__ __forceinline__ int32_t units_of(int32_t len, const PoolView& pv, int32_t units_per_chunk, int32_t unit_tokens = UNIT_TOKENS) {
-  const int32_t Tc = pv.tokens_per_chunk, full = divide(len, pv.by_chunk), rest = len - full * Tc;
-  return full * units_per_chunk + (rest + unit_tokens - 1) / unit_tokens;
-}
-
 // Kernel arguments that a wave needs early. Named in one place, they are asked for together when it starts; left to
 // itself the compiler puts loads of them behind waits for other loads and behind branches, and no cache holds them yet.
 // (eight to an asm statement: across such statements loads are not made into wider ones)

@@ -9,6 +9,7 @@
 #else
 #define ELLM_BOTH
 #endif
+#define ELLM_BOTH_INLINE ELLM_BOTH inline __attribute__((always_inline))
 
 namespace ellm {
 

@@ -45,6 +45,12 @@ struct PoolView {
   Divisor by_chunk, by_tiles, by_units;   // division by tokens_per_chunk, tiles_per_chunk, units_per_chunk
 };
 
+// number of units (tiles) of a sequence of len tokens (neither straddles a chunk)
+ELLM_BOTH_INLINE int32_t units_of(int32_t len, const PoolView& pv, int32_t units_per_chunk, int32_t unit_tokens = UNIT_TOKENS) {
+  const int32_t Tc = pv.tokens_per_chunk, full = divide(len, pv.by_chunk), rest = len - full * Tc;
+  return full * units_per_chunk + (rest + unit_tokens - 1) / unit_tokens;
+}
+
 // One decode launch: requests [q_row0, q_row0 + n_req) of the caller's batch.
 // For every kv head the units of all requests, laid end to end in request order, form one sequence
 // of units_per_head units, which is dealt out evenly to waves_per_head waves: wave w takes

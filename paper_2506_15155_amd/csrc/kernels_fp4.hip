@@ -21,23 +21,9 @@
 // 512 to 24576, 16 q heads of 64, take 30.5 (3.5 TB/s): the vector unit, 60 % busy, between the ramp and the sums of shared requests.
 // The K rows of the next tile are asked for when this one's scores are formed, its V rows when this one's have gone to LDS.
 #include "fp4.hpp"
+#include "fp4_walk.hpp"
 
 namespace ellm {
-
-enum : uint32_t { T_FIRST = 1, T_LAST = 2, T_FIN = 4 };   // a tile starts a request here, ends it, ends the share
-// What is known of a tile before its loads are issued (uniform). RUN: its units are neighbours in one chunk, a tile ends where its
-// chunk does, and one address is enough for all of it; else every unit has an address of its own.
-template <int U, bool RUN>
-struct Fp4Tile {
-  static constexpr int PIECES = RUN ? 1 : U;
-  int32_t n, b, part;                // units, request, partial slot of the request in this wave (-1: finished here)
-  uint32_t flags;                    // T_*
-  int32_t tail;                      // rows of its last unit
-  int32_t rows[PIECES];              // of the run, or of each unit (0: the tile has no such unit)
-  int32_t r[PIECES];                 // first row in its chunk
-  uint32_t at[PIECES];               // the chunk (table entry, or slot of the tensor's own range)
-  const char* base;                  // start of the pool, or of the tensor's range
-};
 
 // V rows of two units on their way through LDS, half of the dims at a time (heads of 64: all): two words, 16 dims, of every quarter.
 // Rows are 32 bytes apart modulo the banks' 128, which keeps the transposing reads (32 bytes of 4 rows at a time) off each
@@ -60,6 +46,16 @@ constexpr int WEIGHT_BITS = 12, VALUE_BITS = 13;
 constexpr float LARGE_SCORE = 0x1p20f;
 // what weights are relative to, for a largest score of `top`
 __device__ __forceinline__ float reference(float top) { return __builtin_fabsf(top) > LARGE_SCORE ? top : top - WEIGHT_BITS; }
+
+// a request's chunks
+template <bool DIRECT>
+struct Fp4Tensor {
+  TensorWalk walk;
+  const char* base;                  // start of the pool, or of the tensor's range
+  Fp4Tensor() = default;
+  __device__ __forceinline__ Fp4Tensor(const PoolView& pv, int32_t tensor) : walk(tensor_walk<DIRECT>(pv, tensor)), base(DIRECT ? walk.tbase : pv.base) {}
+  __device__ __forceinline__ uint32_t chunk(int32_t slot) const { return DIRECT ? (uint32_t)slot : (uint32_t)walk.trow[slot]; }
+};
 
 typedef short __attribute__((ext_vector_type(4))) s16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
@@ -95,80 +91,12 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   const float size = __builtin_fabsf(scale_log2);
   const uint32_t sign = scale_log2 < 0.f ? 0x80008000u : 0u;
 
-  // ---- cursor: the next tile to be asked for ----
-  int32_t cb = sh.b, rem_share = sh.n_units, len, slot, r, rem_req, part;
-  uint32_t first = T_FIRST;
-  TensorWalk walk;
+  using Tensor = Fp4Tensor<DIRECT>;
+  auto open = [&](int32_t tensor) __attribute__((always_inline)) { return Tensor(pv, tensor); };
   const typename Args::Req& first_rq = sh.first;
-  {
-    const typename Args::Req& rq = first_rq;
-    len = rq.len;
-    walk = tensor_walk<DIRECT>(pv, rq.tensor);
-    constexpr int32_t STEP_WAVES = NW ? NW : 1;
-    const int32_t mine = NW ? wave * a.step_units / STEP_WAVES : 0;     // (at most U apart from one wave to the next)
-    const int32_t u0 = (sh.u_lo - rq.unit_prefix) * a.step_units + mine;
-    rem_req = units_of(len, pv, pv.units_per_chunk) - u0;
-    if (NW) rem_share = min((wave + 1) * a.step_units / STEP_WAVES - mine, rem_req);
-    else if (a.step_units > 1) rem_share = min(rem_share * a.step_units, rem_req);
-    slot = divide(u0, pv.by_units);
-    r = (u0 - slot * pv.units_per_chunk) * UNIT_TOKENS;
-    part = rq.n_part == 1 ? -1 : rq.part0 + (sh.w - rq.wave_first);    // (which slot: only where a workgroup is a step)
-  }
-  auto advance = [&](Tile& t) __attribute__((always_inline)) {
-    t.n = min(U, min(rem_share, rem_req));
-    t.b = cb;
-    t.part = part;
-    t.flags = first;
-    t.base = DIRECT ? walk.tbase : pv.base;
-    if constexpr (RUN) {
-      t.n = min(t.n, (Tc - r + UNIT_TOKENS - 1) / UNIT_TOKENS);
-      t.at[0] = DIRECT ? (uint32_t)slot : (uint32_t)walk.trow[slot];
-      t.r[0] = r;
-      t.rows[0] = min(t.n * UNIT_TOKENS, min(Tc - r, len - (slot * Tc + r)));      // (past the end of the share: 0)
-      t.tail = t.rows[0] - (t.n - 1) * UNIT_TOKENS;
-      if (rem_req > t.n) {                             // there is a next unit of this request
-        r += t.n * UNIT_TOKENS;
-        if (r >= Tc) { r = 0; slot += 1; }
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; u++) {
-        if (u == 0 || u < t.n) {
-          t.at[u] = DIRECT ? (uint32_t)slot : (uint32_t)walk.trow[slot];
-          t.r[u] = r;
-          t.rows[u] = min(UNIT_TOKENS, min(Tc - r, len - (slot * Tc + r)));
-          t.tail = t.rows[u];
-          if (u < t.n - 1 || (t.n > 0 && rem_req > t.n)) {   // there is a next unit of this request
-            r += UNIT_TOKENS;
-            if (r >= Tc) { r = 0; slot += 1; }
-          }
-        } else {
-          t.at[u] = t.at[u - 1];
-          t.r[u] = t.r[u - 1];
-          t.rows[u] = 0;
-        }
-      }
-      if (t.n == 0) t.rows[0] = 0;                     // past the end of the share
-    }
-    rem_req -= t.n;
-    rem_share -= t.n;
-    first = 0;
-    if (rem_req == 0) {
-      t.flags |= T_LAST;
-      first = T_FIRST;
-    }
-    if (rem_share == 0) t.flags |= T_FIN;
-    if (rem_req == 0 && rem_share > 0) {
-      cb += 1;
-      const typename Args::Req rq = a.req[cb];
-      len = rq.len;
-      rem_req = units_of(len, pv, pv.units_per_chunk);
-      walk = tensor_walk<DIRECT>(pv, rq.tensor);
-      slot = 0;
-      r = 0;
-      part = rq.n_part == 1 ? -1 : rq.part0;
-    }
-  };
+  Fp4Cursor<U, RUN, Tensor> cursor;
+  cursor.template begin<NW>(pv, a, first_rq, sh.b, sh.w, sh.u_lo, sh.n_units, wave, open);
+  auto advance = [&](Tile& t) __attribute__((always_inline)) { cursor.next(pv, a, open, t); };
   // a piece's K rows and scales (V's: plane, scale_plane further on)
   auto rows_base = [&](const Tile& t, int i) __attribute__((always_inline)) {
     return const_cast<char*>(t.base) + (uint64_t)t.at[i] * pv.chunk_bytes + head_rows + (uint32_t)t.r[i] * ROW;
@@ -176,10 +104,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   auto scales_base = [&](const Tile& t, int i) __attribute__((always_inline)) {
     return const_cast<char*>(t.base) + (uint64_t)t.at[i] * pv.chunk_bytes + head_scales + (uint32_t)t.r[i] * SCALES;
   };
-  // how many of the rows are in the chunk: all but the one that a fused append is about to put there
-  auto there = [&](const Tile& t, int i) __attribute__((always_inline)) {
-    return t.rows[i] - (APPEND && (t.flags & T_LAST) && (RUN || i == t.n - 1) ? 1 : 0);
-  };
+  auto there = [&](const Tile& t, int i) __attribute__((always_inline)) { return t.template there<APPEND>(i); };
   // rows of unit u
   auto rows_of = [&](const Tile& t, int u) __attribute__((always_inline)) {
     return RUN ? min(t.rows[0] - u * UNIT_TOKENS, UNIT_TOKENS) : t.rows[RUN ? 0 : u];
@@ -432,7 +357,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     __shared__ __attribute__((aligned(16))) char lds[NW][MINE];
     __shared__ float2 ml[NW][HEADS];
     float* const mine = reinterpret_cast<float*>(lds[wave]);
-    if (rem_share > 0) {
+    if (cursor.rem_share > 0) {
       Tile t;
       advance(t);
       issue_k(t);
@@ -472,8 +397,8 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       for (int w = 0; w < NW; w++) sum.M = fmaxf(sum.M, p[w].x);
 #pragma unroll
       for (int w = 0; w < NW; w++) add(sum, p[w].y, v4[w], fast_exp2(p[w].x - sum.M));
-      if (part < 0) write_out<D>(pv, out, a, cb, g, g_first, x, sum);
-      else leave_partial<D>(pv, ws, a, part, g, g_first, n_heads, x, sum);
+      if (cursor.part < 0) write_out<D>(pv, out, a, cursor.b, g, g_first, x, sum);
+      else leave_partial<D>(pv, ws, a, cursor.part, g, g_first, n_heads, x, sum);
     }
     // one of several blocks of its request: the last of them to get here adds their results up
     const int32_t n_part = first_rq.n_part;
@@ -485,7 +410,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)n_part - 1u) return;
     Sum all_of[1];
     all.template sum<1, 8, 16>(all_of, x, 0, 0, n_part);
-    if (x < n_cols) write_out<D>(pv, out, a, cb, g, g_first, x, all_of[0]);
+    if (x < n_cols) write_out<D>(pv, out, a, cursor.b, g, g_first, x, all_of[0]);
     return;
   }
   __shared__ __attribute__((aligned(16))) char stages[NW ? 1 : SW][NW ? 1 : STAGE_BYTES];
