@@ -4,8 +4,6 @@
 
 namespace ellm {
 
-ELLM_BOTH_INLINE int32_t least(int32_t a, int32_t b) { return a < b ? a : b; }
-
 enum : uint32_t { T_FIRST = 1, T_LAST = 2, T_FIN = 4 };   // a tile starts a request here, ends it, ends the share
 // What is known of a tile before its loads are issued (uniform). RUN: its units are neighbours in one chunk, a tile ends where its
 // chunk does, and one address is enough for all of it; else every unit has an address of its own.

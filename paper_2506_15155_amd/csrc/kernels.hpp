@@ -45,6 +45,8 @@ struct PoolView {
   Divisor by_chunk, by_tiles, by_units;   // division by tokens_per_chunk, tiles_per_chunk, units_per_chunk
 };
 
+ELLM_BOTH_INLINE int32_t least(int32_t a, int32_t b) { return a < b ? a : b; }
+
 // number of units (tiles) of a sequence of len tokens (neither straddles a chunk)
 ELLM_BOTH_INLINE int32_t units_of(int32_t len, const PoolView& pv, int32_t units_per_chunk, int32_t unit_tokens = UNIT_TOKENS) {
   const int32_t Tc = pv.tokens_per_chunk, full = divide(len, pv.by_chunk), rest = len - full * Tc;
@@ -170,6 +172,13 @@ struct alignas(64) TokenArgs {
   int32_t block0[MAX_LAUNCH_REQ];  // blocks of the requests before this one
 };
 inline int32_t token_blocks(int64_t pos0, int64_t n) { return n > 0 ? (int32_t)((pos0 + n - 1) / TOKEN_BLOCK - pos0 / TOKEN_BLOCK + 1) : 0; }
+// positions p0 .. p1 - 1: those of a request in its block number `block`
+struct TokenRange { int32_t p0, p1; };
+ELLM_BOTH_INLINE TokenRange token_range(int32_t pos0, int32_t n, int32_t block) {
+  const int32_t begin = (pos0 / TOKEN_BLOCK + block) * TOKEN_BLOCK;
+  // (both ends from where the block begins on: the last block of all positions ends at 2^31)
+  return {begin > pos0 ? begin : pos0, begin + least(TOKEN_BLOCK, pos0 - begin + n)};
+}
 
 // Tokens copied from tensors to the ends of others. Copies of the same tokens, neighbours in the call, are a group: its
 // rows are read once and written to all of its destinations. A workgroup takes COPY_BYTES of rows of one kv head.

@@ -54,9 +54,9 @@ __device__ __forceinline__ int32_t find_last(const int32_t* first, int32_t n, in
 // A workgroup's tokens of the dense side: request b, positions p0 .. p1 - 1
 struct TokenShare { int32_t b, p0, p1; };
 __device__ __forceinline__ TokenShare token_share(const TokenArgs& a, int32_t block) {
-  const int32_t b = find_last(a.block0, a.n_req, block), pos0 = a.pos0[b];
-  const int32_t begin = (pos0 / TOKEN_BLOCK + (block - a.block0[b])) * TOKEN_BLOCK;
-  return {b, max(begin, pos0), min(begin + TOKEN_BLOCK, pos0 + a.n[b])};
+  const int32_t b = find_last(a.block0, a.n_req, block);
+  const TokenRange r = token_range(a.pos0[b], a.n[b], block - a.block0[b]);
+  return {b, r.p0, r.p1};
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void fp4_append_kernel(PoolView pv, const char
   const TokenShare s = token_share(a, blockIdx.x);
   const int32_t h = blockIdx.y, rows = s.p1 - s.p0, sub = threadIdx.x % LPR;
   const Tensor<DIRECT> t(pv, a.tensor[s.b]);
-  const int64_t from = ((int64_t)(a.row0[s.b] + s.p0 - a.pos0[s.b]) * pv.n_kv_heads + h) * (2 * D) + sub * 16;
+  const int64_t from = ((int64_t)(a.row0[s.b] + (s.p0 - a.pos0[s.b])) * pv.n_kv_heads + h) * (2 * D) + sub * 16;
   const int64_t token_bytes = (int64_t)pv.n_kv_heads * (2 * D);
   uint4 x[N];
 #pragma unroll
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256) void read_tokens_kernel(PoolView pv, char* __r
   const TokenShare s = token_share(a, blockIdx.x);
   const int32_t h = blockIdx.y, rows = s.p1 - s.p0, sub = threadIdx.x % LPR;
   const Tensor<DIRECT> t(pv, a.tensor[s.b]);
-  const int64_t to = ((int64_t)(a.row0[s.b] + s.p0 - a.pos0[s.b]) * pv.n_kv_heads + h) * (2 * D) + sub * 16;
+  const int64_t to = ((int64_t)(a.row0[s.b] + (s.p0 - a.pos0[s.b])) * pv.n_kv_heads + h) * (2 * D) + sub * 16;
   const int64_t token_bytes = (int64_t)pv.n_kv_heads * (2 * D);
   uint4 x[N];
   uint32_t codes[N], scale[N];
