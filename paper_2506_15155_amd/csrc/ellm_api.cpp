@@ -1107,6 +1107,14 @@ int fits_one_call(ellm_pool* p, int64_t total, const ellm_tensor_id* ids, int32_
   return fits ? ELLM_OK : set_err(ELLM_ERR_RANGE, std::string(call) + ": too many tokens in one call, or in a tensor");
 }
 
+// an append to a pool of 4-bit rows: p->n_eff tokens behind those of each tensor
+int rows_fit(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, const char* call) {
+  for (int32_t i = 0; i < batch && p->geom.fp4; i++)
+    if (p->core->tensor(ids[i])->len + p->n_eff[i] > 0x7fffffffll)
+      return set_err(ELLM_ERR_RANGE, std::string(call) + ": tensors of 4-bit rows hold less than 2^31 tokens");
+  return ELLM_OK;
+}
+
 // Requests b0 .. b0 + nb - 1 of p->n_eff tokens each, at the ends of their tensors (first NULL) or from first[b] on. Returns
 // the dense side's rows of the requests before them.
 int64_t token_args(ellm_pool* p, ellm::TokenArgs& a, const ellm_tensor_id* ids, int32_t b0, int32_t nb, const int64_t* first) {
@@ -1308,7 +1316,7 @@ int ellm_kv_append(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, const
   if (rc) return rc;
   if (total > 0 && (!k_new || !v_new)) return set_err(ELLM_ERR_INVALID, "kv_append: NULL k_new / v_new");
   if (total > 0x7fffffffll / (2 * p->geom.n_kv_heads)) return set_err(ELLM_ERR_RANGE, "kv_append: too many tokens in one call");
-  if (p->geom.fp4 && (rc = fits_one_call(p, total, ids, batch, "kv_append"))) return rc;
+  if ((rc = rows_fit(p, ids, batch, "kv_append"))) return rc;
   if (total == 0) return ELLM_OK;
   hipStream_t stream = (hipStream_t)stream_;
   int32_t most_new = 0;
@@ -1676,6 +1684,7 @@ int ellm_kv_append_decode(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch
   int rc = core_err(p, p->core->append_check(ids, batch, nullptr, p->n_eff, nullptr));
   if (rc) return rc;
   if (batch > 0 && (!k_new || !v_new)) return set_err(ELLM_ERR_INVALID, "kv_append_decode: NULL k_new / v_new");
+  if ((rc = rows_fit(p, ids, batch, "kv_append_decode"))) return rc;
   rc = core_err(p, p->core->decode_check(ids, batch, 1));
   if (rc) return rc;
   if (batch == 0) return ELLM_OK;

@@ -5,6 +5,8 @@ import subprocess
 
 import pytest
 
+import paper_2506_15155_amd as E
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PROGRAM = r"""
 #include "kernels.hpp"
@@ -47,3 +49,24 @@ def test_every_position_once(tmp_path):
                     "-I", os.path.join(ROOT, "paper_2506_15155_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     wrong, blocks = map(int, subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split())
     assert wrong == 0 and blocks > 100_000
+
+
+def test_the_fused_append_refuses_what_the_append_refuses():
+    """Tensors of 4-bit rows hold less than 2^31 tokens, whichever call brings the last one, and whatever the call's other tensors get."""
+    cb = 1 << 31
+    p = E.ellm_pool_create(None, None, cb, 1, 1, 64, 2, 400, flags=E.ELLM_POOL_METADATA_ONLY, device_bytes=800 * cb, dtype=E.ELLM_MXFP4)
+    T = E.ellm_pool_get_geometry(p)["tokens_per_chunk"]
+    t, other = E.ellm_tensor_create(p, 3 << 30), E.ellm_tensor_create(p, 2 * T)
+    E.ellm_tensor_map_chunks(p, t, 0, -(-(3 << 30) // T))
+    E.ellm_tensor_map_chunks(p, other, 0, 2)
+    append = lambda ids, n: E.ellm_kv_append(p, ids, 16, 16, n, check=False)  # noqa: E731
+    fused = lambda ids: E.ellm_kv_append_decode(p, ids, 16, 16, 16, 16, check=False)  # noqa: E731
+    length = lambda x: E.ellm_tensor_get_table(p, x)[1]  # noqa: E731
+    assert append([t], [(1 << 30) - 1]) == append([t], [(1 << 30) - 1]) == 0
+    # 2^31 - 2 tokens: one more is taken, whether others come with it or not
+    assert fused([other, t]) == E.ERR.NO_DEVICE
+    assert append([t, other], [1, 500]) == 0 and length(t) == (1 << 31) - 1 and length(other) == 500
+    assert append([other, t], [1, 1]) == fused([t]) == fused([other, t]) == E.ERR.RANGE and "2^31" in E.ellm_last_error()
+    assert fused([other]) == E.ERR.NO_DEVICE
+    assert length(t) == (1 << 31) - 1 and length(other) == 500
+    E.ellm_pool_destroy(p)
