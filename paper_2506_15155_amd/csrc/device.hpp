@@ -339,9 +339,34 @@ __device__ __forceinline__ void rescale(Sum& s, float M) {
   s.A.x *= w; s.A.y *= w; s.A.z *= w; s.A.w *= w;
 }
 
+// The same where the rows are means (sums divided by their L): the sum is one as well, so no weight of V's row is over 1 and nothing is
+// out of range that V is not. A part of no weight at all (L of 0: every score -inf) has a row of zeros.
+// (the reciprocal instruction, to 2^-23: weights are held to fewer bits, and L is never near the ends of a float's range)
+__device__ __forceinline__ float share_of(float L) { return L == 0.f ? 0.f : __builtin_amdgcn_rcpf(L); }
+template <int N>        // a power of two
+__device__ __forceinline__ void add_means(Sum& s, float M, const float (&L)[N], const float4 (&v)[N], float (&w)[N]) {
+  const float before = s.L * fast_exp2(s.M - M);
+  float sums[N];                     // (pairs first: everything waits for it)
+#pragma unroll
+  for (int u = 0; u < N; u++) sums[u] = w[u] *= L[u];
+#pragma unroll
+  for (int n = N / 2; n > 0; n /= 2)
+#pragma unroll
+    for (int u = 0; u < n; u++) sums[u] += sums[u + n];
+  const float all = before + sums[0], share = share_of(all), keep = before * share;
+  s.M = M;
+  s.L = all;
+  s.A.x *= keep; s.A.y *= keep; s.A.z *= keep; s.A.w *= keep;
+#pragma unroll
+  for (int u = 0; u < N; u++) {
+    const float c = w[u] * share;
+    s.A.x += v[u].x * c; s.A.y += v[u].y * c; s.A.z += v[u].z * c; s.A.w += v[u].w * c;
+  }
+}
+
 // The partials of a request for n_heads q heads of kv head g from head g_first of the group on. Columns: the pieces of
-// the heads' rows in order.
-template <int D>
+// the heads' rows in order. MEANS: their rows are means.
+template <int D, bool MEANS = false>
 struct Partials {
   static constexpr int F = D / 4;
   __amdgpu_buffer_rsrc_t rows, pairs;
@@ -380,6 +405,19 @@ struct Partials {
         float M = sums[k].M;
 #pragma unroll
         for (int u = 0; u < N; u++) M = j0 + u < j1 ? fmaxf(M, __uint_as_float(ml[k][u].x)) : M;
+        if constexpr (MEANS) {
+          float L[N], w[N];
+          float4 rows_of[N];
+#pragma unroll
+          for (int u = 0; u < N; u++) {
+            const words4_t t = v[k][u];
+            L[u] = __uint_as_float(ml[k][u].y);
+            rows_of[u] = make_float4(__uint_as_float(t.x), __uint_as_float(t.y), __uint_as_float(t.z), __uint_as_float(t.w));
+            w[u] = j0 + u < j1 ? fast_exp2(__uint_as_float(ml[k][u].x) - M) : 0.f;
+          }
+          add_means(sums[k], M, L, rows_of, w);
+          continue;
+        }
         rescale(sums[k], M);
 #pragma unroll
         for (int u = 0; u < N; u++) {
@@ -396,11 +434,12 @@ struct Partials {
 };
 
 // column x of request b's output: the four dims that piece x % (D / 4) of the rows holds, of head g_first + x / (D / 4)
-template <int D, class Args>
+template <int D, bool MEANS = false, class Args>
 __device__ __forceinline__ void write_out(const PoolView& pv, uint16_t* __restrict__ out, const Args& a, int32_t b, int32_t g,
                                           int32_t g_first, int32_t x, const Sum& s) {
   constexpr int F = D / 4;
-  const float inv = 1.f / s.L;
+  // (no weight at all: 0 / 0, as the sums would have it)
+  const float inv = MEANS ? s.L == 0.f ? __builtin_nanf("") : 1.f : 1.f / s.L;
   uint16_t* o = out + ((int64_t)(a.q_row0 + b) * pv.n_q_heads + g * pv.group + g_first + x / F) * D + partial_dim<D>(a.unit_tokens, x % F);
   *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(s.A.x * inv, s.A.y * inv), pack_bf16(s.A.z * inv, s.A.w * inv));
 }
@@ -448,7 +487,8 @@ __device__ __forceinline__ void leave_partial(const PoolView& pv, float* ws, con
 // wave for a request and branches around the parts of each sum: 48 requests of 6 q heads each 49.95 -> 49.3 us, 64 of 16
 // heads of 64 66.4 -> 65.7, chunks of 16 tokens 33.6 -> 33.3, the 8B-shaped step 1995 -> 1985.
 // ONE, TWO: how many partial results a lane asks for at a time where it adds up one column, or two.
-template <int D, int HEADS, int ONE = 16, int TWO = 8, class Args>
+// MEANS: of what the rows are (Partials)
+template <int D, int HEADS, int ONE = 16, int TWO = 8, bool MEANS = false, class Args>
 __device__ __forceinline__ void end_shares(const PoolView& pv, float* ws_, uint16_t* __restrict__ out, const Args& a, const Records<Args>& records,
                                            const Results<D, HEADS>& res, int32_t g_first, int32_t n_heads, int32_t workgroup, int32_t wave, int32_t lane) {
   constexpr int F = D / 4, SLOTS = Results<D, HEADS>::SLOTS, NONE = Results<D, HEADS>::NONE;
@@ -500,10 +540,20 @@ __device__ __forceinline__ void end_shares(const PoolView& pv, float* ws_, uint1
       Sum s = {ml[0].x, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
       for (int i = 1; i < SHARE_WAVES; i++) s.M = fmaxf(s.M, ml[i].x);
+      if constexpr (MEANS) {
+        float L[SHARE_WAVES], w[SHARE_WAVES];
 #pragma unroll
-      for (int i = 0; i < SHARE_WAVES; i++) add(s, ml[i].y, v[i], fast_exp2(ml[i].x - s.M));
+        for (int i = 0; i < SHARE_WAVES; i++) {
+          L[i] = ml[i].y;
+          w[i] = fast_exp2(ml[i].x - s.M);
+        }
+        add_means(s, s.M, L, v, w);
+      } else {
+#pragma unroll
+        for (int i = 0; i < SHARE_WAVES; i++) add(s, ml[i].y, v[i], fast_exp2(ml[i].x - s.M));
+      }
       if (whole) {
-        if (x < h1 * F) write_out<D>(pv, out, a, b, g, g_first, x, s);
+        if (x < h1 * F) write_out<D, MEANS>(pv, out, a, b, g, g_first, x, s);
       } else {
         store_partial(rows, x * 16, s.A);
         if (f == 0) store_partial(pairs, x / F * (WS_ML * 4), make_float2(s.M, s.L));
@@ -513,12 +563,12 @@ __device__ __forceinline__ void end_shares(const PoolView& pv, float* ws_, uint1
     stores_done();
     uint32_t before = 0;
     if (lane < n_pieces) before = count_in(pv, g * MAX_LAUNCH_REQ + b, p0 + lane, parts.n);
-    const Partials<D> all(ws, ws_slots, slot0, parts.n, held(pv.group), g_first, h1);
+    const Partials<D, MEANS> all(ws, ws_slots, slot0, parts.n, held(pv.group), g_first, h1);
     // (all of a wave's pieces or none, as a rule)
     const uint32_t last = (uint32_t)__builtin_amdgcn_ballot_w64(lane < n_pieces && before == (uint32_t)parts.n - 1u);
     if (!last) continue;
     auto done = [&](int32_t x, const Sum& s) __attribute__((always_inline)) {
-      if (x < h1 * F && (last >> ((x / F >> shift) - p0) & 1u)) write_out<D>(pv, out, a, b, g, g_first, x, s);
+      if (x < h1 * F && (last >> ((x / F >> shift) - p0) & 1u)) write_out<D, MEANS>(pv, out, a, b, g, g_first, x, s);
     };
     const int32_t x = h0 * F + lane;
     if ((h1 - h0) * F <= 64) {

@@ -1639,8 +1639,8 @@ static int decode_impl(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, c
     *n_launched += pair ? batch : launches[i].n_req;
     if (prof) p->prof_used++;
     for (int h = 0; h < (pair ? 2 : 1) && !err; h++) {
-      e = pair ? ellm::launch_decode_combine(pv, ws + (h ? p->pair.floats : 0), out, p->pair.half[h], stream)
-               : ellm::launch_decode_combine(pv, ws, out, launches[i], stream);
+      e = pair ? ellm::launch_decode_combine(pv, ws + (h ? p->pair.floats : 0), out, p->pair.half[h], p->geom.fp4, stream)
+               : ellm::launch_decode_combine(pv, ws, out, launches[i], p->geom.fp4, stream);
       if (e) err = hip_err((hipError_t)e, "decode combine launch");
     }
   }

@@ -1026,11 +1026,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // waves are slower below 64 partials (32: 11.7 a call, 11.2; of heads of 64 36: 9.5, 8.4), faster for many (256 of heads
 // of 64: 19.5, 21.5). In a launch in blocks a request that the attention kernel would have added up, were it not for
 // another request, is added up in that kernel's order: its bits do not depend on its neighbours (IN_ORDER; its registers are as many
-// as 16 partials ahead take, which launches of many workgroups do not have to pay).
+// as 16 partials ahead take, which launches of many workgroups do not have to pay). MEANS: of what the rows are (Partials).
 // ---------------------------------------------------------------------------------------------
 constexpr int COMBINE_AHEAD = 4;     // rows a lane asks for before it waits
 
-template <int D, int W, bool IN_ORDER = false>
+template <int D, int W, bool IN_ORDER, bool MEANS>
 __global__ __launch_bounds__(64 * W) void decode_combine_kernel(const float* __restrict__ ws, uint16_t* __restrict__ out,
                                                                 int32_t n_q_heads, int32_t group, BatchArgs a) {
   constexpr int F = D / 4, RP = W * 64 / F, AHEAD = COMBINE_AHEAD;
@@ -1044,10 +1044,10 @@ __global__ __launch_bounds__(64 * W) void decode_combine_kernel(const float* __r
     pv.n_q_heads = n_q_heads;
     pv.group = group;
     if (threadIdx.x >= F) return;
-    const Partials<D> all(ws, a.ws_slots, (int64_t)g * a.parts_per_head + a.req[b].part0, n_part, group, h - g * group, 1);
+    const Partials<D, MEANS> all(ws, a.ws_slots, (int64_t)g * a.parts_per_head + a.req[b].part0, n_part, group, h - g * group, 1);
     Sum s[1];
     all.template sum<1, 8, 16>(s, f, 0, 0, n_part);
-    write_out<D>(pv, out, a, b, g, h - g * group, f, s[0]);
+    write_out<D, MEANS>(pv, out, a, b, g, h - g * group, f, s[0]);
     return;
   }
   const int64_t row0 = ((int64_t)g * a.parts_per_head + a.req[b].part0) * group + (h - g * group);
@@ -1055,14 +1055,16 @@ __global__ __launch_bounds__(64 * W) void decode_combine_kernel(const float* __r
   const float* q0 = ws + (int64_t)a.ws_slots * group * D + row0 * WS_ML;      // their (m, l) pairs
   const int64_t stride = (int64_t)group * F, qstride = (int64_t)group * WS_ML;
   float4 v[AHEAD];
-  float mv[AHEAD];
+  float mv[AHEAD], lv[AHEAD];
 #pragma unroll
   for (int u = 0; u < AHEAD; u++) {
     const int j = row + u * RP;
     mv[u] = -INFINITY;
+    lv[u] = 0.f;
     v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (j < n_part) {
       mv[u] = q0[j * qstride];
+      if (MEANS) lv[u] = q0[j * qstride + 1];
       v[u] = p[j * stride];
     }
   }
@@ -1072,14 +1074,17 @@ __global__ __launch_bounds__(64 * W) void decode_combine_kernel(const float* __r
   M = wave_max(M);
   for (int j = lane; j < n_part; j += 64) L += q0[j * qstride + 1] * fast_exp2(q0[j * qstride] - M);
   L = wave_sum(L);
+  const float share = MEANS ? share_of(L) : 0.f;
+  // what a row counts: its part's weight, of sums as they are, of means as a share of the whole
+  auto weight = [&](float m, float l) __attribute__((always_inline)) { return MEANS ? fast_exp2(m - M) * l * share : fast_exp2(m - M); };
   float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](const float4& x, float c) __attribute__((always_inline)) {
     A.x += x.x * c; A.y += x.y * c; A.z += x.z * c; A.w += x.w * c;
   };
 #pragma unroll
   for (int u = 0; u < AHEAD; u++)
-    if (row + u * RP < n_part) add(v[u], fast_exp2(mv[u] - M));
-  for (int j = row + AHEAD * RP; j < n_part; j += RP) add(p[j * stride], fast_exp2(q0[j * qstride] - M));
+    if (row + u * RP < n_part) add(v[u], weight(mv[u], lv[u]));
+  for (int j = row + AHEAD * RP; j < n_part; j += RP) add(p[j * stride], weight(q0[j * qstride], MEANS ? q0[j * qstride + 1] : 0.f));
   sums[row][f] = A;
   __syncthreads();
   if (row != 0) return;
@@ -1087,6 +1092,7 @@ __global__ __launch_bounds__(64 * W) void decode_combine_kernel(const float* __r
 #pragma unroll 8
   for (int r = 1; r < RP; r++) add(sums[r][f], 1.f);
   uint16_t* o = out + ((int64_t)(a.q_row0 + b) * n_q_heads + h) * D + partial_dim<D>(a.unit_tokens, f);
+  if (MEANS) L = L == 0.f ? __builtin_nanf("") : 1.f;
   *reinterpret_cast<uint2*>(o) = make_uint2(f32_to_bf16_bits(A.x / L) | (f32_to_bf16_bits(A.y / L) << 16),
                                             f32_to_bf16_bits(A.z / L) | (f32_to_bf16_bits(A.w / L) << 16));
 }
@@ -1337,7 +1343,7 @@ int launch_decode_pair(const PoolView& pv, const void* q, const void* k_new, con
   return launch_partial(pv, q, k_new, v_new, ws, out, scale_log2, a.half[0], a, a.workgroups + workgroups_of(pv, a.half[1]), stream, ev_start, ev_stop);
 }
 
-int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const BatchArgs& a, hipStream_t stream) {
+int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const BatchArgs& a, bool means, hipStream_t stream) {
   if (a.n_req <= 0 || a.n_split_req <= 0) return 0;
   // where every wave leaves partials there can be few of them each for many requests: as many waves as these fill
   const bool single = a.wg_waves == 1 && a.step_units <= STEP_UNITS;
@@ -1345,10 +1351,15 @@ int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const 
   auto go = [&](auto kernel, unsigned waves) {
     return launch(kernel, dim3(a.n_split_req, pv.n_q_heads), 64 * waves, stream, ws, (uint16_t*)out, pv.n_q_heads, pv.group, a);
   };
-  if (a.in_order_parts) return pv.head_dim == 128 ? go(decode_combine_kernel<128, 8, true>, 8) : go(decode_combine_kernel<64, 4, true>, 4);
-  if (pv.head_dim == 128)
-    return fill < 1 ? go(decode_combine_kernel<128, 2>, 2) : fill < 4 ? go(decode_combine_kernel<128, 4>, 4) : go(decode_combine_kernel<128, 8>, 8);
-  return fill < 1 ? go(decode_combine_kernel<64, 1>, 1) : go(decode_combine_kernel<64, 4>, 4);
+  auto of_rows = [&](auto kind) {
+    constexpr bool MEANS = decltype(kind)::value;
+    if (a.in_order_parts) return pv.head_dim == 128 ? go(decode_combine_kernel<128, 8, true, MEANS>, 8) : go(decode_combine_kernel<64, 4, true, MEANS>, 4);
+    if (pv.head_dim == 128)
+      return fill < 1 ? go(decode_combine_kernel<128, 2, false, MEANS>, 2)
+             : fill < 4 ? go(decode_combine_kernel<128, 4, false, MEANS>, 4) : go(decode_combine_kernel<128, 8, false, MEANS>, 8);
+    return fill < 1 ? go(decode_combine_kernel<64, 1, false, MEANS>, 1) : go(decode_combine_kernel<64, 4, false, MEANS>, 4);
+  };
+  return means ? of_rows(std::true_type{}) : of_rows(std::false_type{});
 }
 
 int launch_copy(void* dst, const void* src, int64_t bytes, hipStream_t stream) {

@@ -71,7 +71,7 @@ ELLM_BOTH_INLINE int32_t units_of(int32_t len, const PoolView& pv, int32_t units
 // so results do not depend on which wave ran when.
 //
 // Workspace of a launch, from the pointer the launch is given: accumulator rows
-// [kv head][partial slot of the head][q head of the group][D] fp32 (ws_slots = n_kv_heads *
+// [kv head][partial slot of the head][q head of the group][D] fp32 (4-bit rows: divided by their l; ws_slots = n_kv_heads *
 // parts_per_head slots in all), then the (m, l) pairs in the same order, WS_ML floats each.
 template <int REQS>
 struct BatchArgsOf {
@@ -348,7 +348,8 @@ int launch_decode_partial(const PoolView& pv, const void* q, const void* k_new, 
 // the two plans of `a`, which run the same kernel, in one launch
 int launch_decode_pair(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,
                        PairArgs& a, hipStream_t stream, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
-int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const BatchArgs& a, hipStream_t stream);
+// means: the partial results' rows are means and not sums (4-bit rows)
+int launch_decode_combine(const PoolView& pv, const float* ws, void* out, const BatchArgs& a, bool means, hipStream_t stream);
 
 // ---- rows in 4 bits (fp4.hpp) ----
 int launch_fp4_append(const PoolView& pv, const void* k_new, const void* v_new, const TokenArgs& a, hipStream_t stream);

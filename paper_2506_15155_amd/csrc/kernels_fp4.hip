@@ -333,12 +333,14 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       }
     }
   };
-  // the sums as they are without `largest`, when a request or the share ends
-  auto whole = [&]() __attribute__((always_inline)) {
+  // When a request or the share ends: the sums become means, of weights that are `inv` of what was added up, and get V's scale back, in
+  // this order: V may be as large as floats are, and the sums are up to 2^WEIGHT_BITS for every token of that.
+  auto means = [&](float inv) __attribute__((always_inline)) {
 #pragma unroll
     for (int n = 0; n < NB; n++)
 #pragma unroll
-      for (int i = 0; i < 4; i++) acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i], __builtin_amdgcn_readlane((int)largest - (127 + VALUE_BITS), n / (W / 2)));
+      for (int i = 0; i < 4; i++)
+        acc[n][i] = __builtin_amdgcn_ldexpf(acc[n][i] * inv, __builtin_amdgcn_readlane((int)largest - (127 + VALUE_BITS), n / (W / 2)));
   };
   // which piece of a row, in the order of partial_dim() for units, has dims 16 n + 4 g16 .. + 3
   auto piece = [&](int n) __attribute__((always_inline)) {
@@ -365,8 +367,8 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       __builtin_amdgcn_sched_barrier(0);
       scores(t);
       weigh(t, lds[wave]);
-      whole();
       const float L = add_xor32(add_xor16(l));
+      means(share_of(L));
       if (c < n_heads) {
 #pragma unroll
         for (int n = 0; n < NB; n++)
@@ -395,9 +397,14 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
       }
 #pragma unroll
       for (int w = 0; w < NW; w++) sum.M = fmaxf(sum.M, p[w].x);
+      float L[NW], weight[NW];
 #pragma unroll
-      for (int w = 0; w < NW; w++) add(sum, p[w].y, v4[w], fast_exp2(p[w].x - sum.M));
-      if (cursor.part < 0) write_out<D>(pv, out, a, cursor.b, g, g_first, x, sum);
+      for (int w = 0; w < NW; w++) {
+        L[w] = p[w].y;
+        weight[w] = fast_exp2(p[w].x - sum.M);
+      }
+      add_means(sum, sum.M, L, v4, weight);
+      if (cursor.part < 0) write_out<D, true>(pv, out, a, cursor.b, g, g_first, x, sum);
       else leave_partial<D>(pv, ws, a, cursor.part, g, g_first, n_heads, x, sum);
     }
     // one of several blocks of its request: the last of them to get here adds their results up
@@ -406,27 +413,26 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
     stores_done();
     uint32_t before = 0;
     if (lane == 0) before = count_in(pv, g * a.waves_per_head + first_rq.wave_first + wave % n_part, wave, n_part);
-    const Partials<D> all(ws, a.ws_slots, (int64_t)g * a.parts_per_head + first_rq.part0, n_part, held(pv.group), g_first, n_heads);
+    const Partials<D, true> all(ws, a.ws_slots, (int64_t)g * a.parts_per_head + first_rq.part0, n_part, held(pv.group), g_first, n_heads);
     if (__builtin_amdgcn_readfirstlane(before) != (uint32_t)n_part - 1u) return;
     Sum all_of[1];
     all.template sum<1, 8, 16>(all_of, x, 0, 0, n_part);
-    if (x < n_cols) write_out<D>(pv, out, a, cursor.b, g, g_first, x, all_of[0]);
+    if (x < n_cols) write_out<D, true>(pv, out, a, cursor.b, g, g_first, x, all_of[0]);
     return;
   }
   __shared__ __attribute__((aligned(16))) char stages[NW ? 1 : SW][NW ? 1 : STAGE_BYTES];
   __shared__ __attribute__((aligned(16))) Results<D, SW == 1 ? 1 : HEADS> results;     // (SW == 1: not used)
   char* const stage = stages[NW ? 0 : wave];
   auto finish = [&](const Tile& t) __attribute__((always_inline)) {
-    whole();
     const float L = add_xor32(add_xor16(l));
+    means(t.part < 0 ? __builtin_amdgcn_rcpf(L) : share_of(L));
     if (c >= n_heads) return;
     if (t.part < 0) {
-      // the whole request lay inside this wave's share: normalise, round and write the output rows
-      const float inv = 1.f / L;
+      // the whole request lay inside this wave's share: round and write the output rows
       uint16_t* o = out + ((int64_t)(a.q_row0 + t.b) * pv.n_q_heads + hq0 + c) * D + 4 * g16;
 #pragma unroll
       for (int n = 0; n < NB; n++)
-        *reinterpret_cast<uint2*>(o + 16 * n) = make_uint2(pack_bf16(acc[n][0] * inv, acc[n][1] * inv), pack_bf16(acc[n][2] * inv, acc[n][3] * inv));
+        *reinterpret_cast<uint2*>(o + 16 * n) = make_uint2(pack_bf16(acc[n][0], acc[n][1]), pack_bf16(acc[n][2], acc[n][3]));
     } else if constexpr (SW == 1) {
       // one of several waves of the request: a partial result
       const int64_t row = ((int64_t)g * a.parts_per_head + t.part) * pv.group + g_first + c;
@@ -470,7 +476,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
   } else if constexpr (SW > 1) {
     results.clear(wave, lane);
   }
-  if constexpr (SW > 1) end_shares<D, HEADS, 8, 4>(pv, ws, out, a, records, results, g_first, n_heads, workgroup, wave, lane);
+  if constexpr (SW > 1) end_shares<D, HEADS, 8, 4, true>(pv, ws, out, a, records, results, g_first, n_heads, workgroup, wave, lane);
 }
 
 template <int D, int U, int HEADS, int SW, bool RUN, bool APPEND, bool DIRECT, class Args>
