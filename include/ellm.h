@@ -506,8 +506,8 @@ int ellm_debug_combined_requests(ellm_pool* pool, const ellm_tensor_id* ids, int
 /* Override the tokens per wave (rounded down to whole 64-token tiles, at least one; 0 = automatic:
  * one wave per SIMD of the GPU). For tests that compare partitions. While an override (this one or
  * ellm_debug_set_waves) is in force, a decode call whose partition needs more partial results than
- * the workspace holds replaces the workspace, which waits for the device; without an override that
- * cannot happen. */
+ * the workspace holds allocates a larger one, which may wait for the device; without an override that
+ * cannot happen. The one before it is freed with the pool, so that graphs captured with it can be replayed. */
 int ellm_pool_set_split_tokens(ellm_pool* pool, int32_t split_tokens);
 
 /* Measurement hooks. profile_enable(max_records > 0) makes each decode launch attach a pair of

@@ -85,6 +85,7 @@ struct ellm_pool {
   size_t merged_words = 0;             // each, two (see PairArgs) for each workspace a launch's partial results can be in
   float* d_ws = nullptr;               // partial results of one decode launch (see BatchArgs)
   int64_t ws_cap_slots = 0;            // partial slots it holds
+  std::vector<float*> old_ws;          // those it took the place of (see ensure_workspace)
   float* static_ws = nullptr;          // this device's copy of the library's fixed workspace
   int64_t static_ws_slots = 0;
   hipStream_t side_in = nullptr;       // fetches (host -> device)
@@ -839,17 +840,17 @@ void vmm_teardown(ellm_pool* p) {
 
 // Under the automatic partition a launch never needs more partial slots than the workspace was
 // sized for. With a partition override in force (tests and measurements) it may: then, and only
-// then, the workspace is replaced by a larger one, which waits for the device.
+// then, a larger one takes the workspace's place, which is kept as long as the pool: graphs captured before write there.
 int ensure_workspace(ellm_pool* p, int64_t n_slots) {
   if (n_slots <= p->ws_cap_slots) return ELLM_OK;
   if (p->split_override <= 0 && p->waves_percent == 100)
     return set_err(ELLM_ERR_RANGE, "decode_attention: launch needs more partial slots than ellm_workspace_bytes allows for");
-  HIP_TRY(hipDeviceSynchronize(), "hipDeviceSynchronize(workspace growth)");
-  HIP_TRY(hipFree(p->d_ws), "hipFree(workspace)");
-  p->d_ws = nullptr;
-  p->ws_cap_slots = 0;
   const int64_t grow = n_slots + n_slots / 4;
-  HIP_TRY(hipMalloc((void**)&p->d_ws, (size_t)grow * slot_bytes(p->geom.group, p->geom.head_dim)), "hipMalloc(workspace)");
+  float* larger = nullptr;
+  p->old_ws.reserve(p->old_ws.size() + 1);
+  HIP_TRY(hipMalloc((void**)&larger, (size_t)grow * slot_bytes(p->geom.group, p->geom.head_dim)), "hipMalloc(workspace)");
+  p->old_ws.push_back(p->d_ws);
+  p->d_ws = larger;
   p->ws_cap_slots = grow;
   return ELLM_OK;
 }
@@ -1263,6 +1264,7 @@ int ellm_pool_destroy(ellm_pool* p) {
     if (p->ev_switch) (void)hipEventDestroy(p->ev_switch);
     for (hipEvent_t e : p->prof_ev) (void)hipEventDestroy(e);
     if (p->d_ws) (void)hipFree(p->d_ws);
+    for (float* ws : p->old_ws) (void)hipFree(ws);
     if (p->d_vbase) (void)hipFree(p->d_vbase);
   }
   if (p->vmm) {
