@@ -191,7 +191,8 @@ int ellm_pool_prepare(ellm_pool* pool, void* stream);
 /* Put the counters of partial results (see ellm_decode_attention) back to 0, on `stream`, behind the pool's append /
  * decode calls so far and before those to come. Needed only after calls have overlapped that must not; the caller
  * sees to it that no replay of a graph that holds decode calls of the pool is in flight. Does not wait for the device. No-op
- * before the pool has its device-side metadata. Errors: INVALID while `stream` or the stream of the
+ * before the pool has its device-side metadata. Also ends the refusals that a move left out by ellm_kv_compact leads to, whose tensor
+ * is best destroyed, or cut to the tokens before those that moved. Errors: INVALID while `stream` or the stream of the
  * pool's last call is being captured; HIP. */
 int ellm_pool_reset_counters(ellm_pool* pool, void* stream);
 
@@ -348,7 +349,9 @@ int ellm_kv_copy(ellm_pool* pool, const ellm_tensor_id* src, const ellm_tensor_i
  *   keep is read by the launch. Positions that break the rules above make the rows behind first[b] undefined, and touch nothing else.
  *   Enqueued on `stream`; returns without waiting. Large moves keep flags in the pool's workspace of partial results: calls are put in
  *   order, but replays of graphs that hold this call must not overlap another replay or call of it, ellm_decode_attention or
- *   ellm_kv_append_decode on the same pool.
+ *   ellm_kv_append_decode on the same pool. Where that happens all the same, outputs and moved rows are undefined; a part of a move that
+ *   waits for flags for seconds is left out, and every later call that would launch a kernel on the pool, and ellm_pool_sync, returns
+ *   HIP (the text names the tensor) until ellm_pool_reset_counters.
  * Checks: unknown flag, batch < 0 -> INVALID; per request in order: bad or repeated handle, negative position or count -> INVALID;
  * first > len, n_keep > len - first -> RANGE; with n_keep > 0 the slots of first .. len - 1 ascending: empty -> UNMAPPED, on host ->
  * NOT_RESIDENT. NULL keep with tokens to keep -> INVALID; 2^30 / n_kv_heads of them or more -> RANGE. Works in one launch per 128
@@ -544,6 +547,10 @@ int ellm_debug_set_compute_units(ellm_pool* pool, int32_t n);
 /* Test hook: every counter of partial results (see ellm_decode_attention) set to value, ordered like
  * ellm_pool_reset_counters' 0. INVALID before the pool has its device-side metadata. */
 int ellm_debug_set_counters(ellm_pool* pool, uint32_t value, void* stream);
+
+/* Test hook: waits inside ellm_kv_compact's kernel look n times for what they wait for before they give up (0: not at all, as if it
+ * never came; -1, the default: for some seconds). */
+int ellm_debug_set_compact_looks(ellm_pool* pool, int32_t n);
 
 /* Measurement only: what the paper's own mechanism costs on this GPU (Sec. 2.1.1, Sec. 3.2: chunks
  * mapped into a reserved virtual range through the driver's virtual-memory calls). Creates

@@ -119,6 +119,7 @@ _sigs = {
     "ellm_debug_compute_beside_copies": [_vp],
     "ellm_pool_reset_counters": [_vp, _vp],
     "ellm_debug_set_counters": [_vp, C.c_uint32, _vp],
+    "ellm_debug_set_compact_looks": [_vp, C.c_int32],
     "ellm_debug_copy": [_vp, _vp, C.c_uint64, _vp],
     "ellm_debug_stream_read": [_vp, C.c_uint64, _vp, _vp],
     "ellm_debug_kv_stream_read": [_vp, _i32p, C.c_int32, _vp, _vp],
@@ -484,6 +485,10 @@ def ellm_pool_get_mapping_stats(pool):
     nm, um, nu, uu = C.c_int64(), C.c_double(), C.c_int64(), C.c_double()
     _ret(lib.ellm_pool_get_mapping_stats(pool, C.byref(nm), C.byref(um), C.byref(nu), C.byref(uu)), True)
     return {"maps": nm.value, "us_map": um.value, "unmaps": nu.value, "us_unmap": uu.value}
+
+
+def ellm_debug_set_compact_looks(pool, n, check=True):
+    return _ret(lib.ellm_debug_set_compact_looks(pool, int(n)), check)
 
 
 def ellm_debug_set_table_kernels(pool, on, check=True):

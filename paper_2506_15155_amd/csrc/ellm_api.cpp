@@ -136,6 +136,12 @@ struct ellm_pool {
   // that a compute call walks a tensor's slots once per change and not once per call.
   struct CopySeen { uint32_t row_version = 0; bool valid = false; int64_t in = 0, out = 0; };
   std::vector<CopySeen> copy_seen;
+  // Waits of ellm_kv_compact's kernel: how often they look at a flag (some seconds), and where one that gives up says so, a
+  // tensor's handle + 1 (host memory that the GPU writes)
+  static constexpr int32_t COMPACT_LOOKS = 1 << 22;
+  int32_t compact_looks = COMPACT_LOOKS;
+  uint32_t* gave_up = nullptr;
+  uint32_t* gave_up_dev = nullptr;     // as the GPU addresses it
   int32_t fail_launch_in = 0;          // debug: the n-th launch from now fails without launching (0 = off)
 
   // Driver-mapped pools (ELLM_POOL_DRIVER_MAPPED): the chunks are physical allocations of the
@@ -297,6 +303,9 @@ int ensure_device(ellm_pool* p) {
       (void)hipGetLastError();
     }
   }
+  HIP_TRY(hipHostMalloc((void**)&p->gave_up, sizeof(uint32_t), hipHostMallocMapped), "hipHostMalloc(mark)");
+  *p->gave_up = 0;
+  HIP_TRY(hipHostGetDevicePointer((void**)&p->gave_up_dev, p->gave_up, 0), "hipHostGetDevicePointer(mark)");
   HIP_TRY(hipStreamCreateWithFlags(&p->side_in, hipStreamNonBlocking), "hipStreamCreate(side)");
   HIP_TRY(hipStreamCreateWithFlags(&p->side_out, hipStreamNonBlocking), "hipStreamCreate(side)");
   HIP_TRY(hipEventCreateWithFlags(&p->ev_switch, hipEventDisableTiming), "hipEventCreate");
@@ -332,6 +341,15 @@ int ensure_device(ellm_pool* p) {
   }
   p->dev_ready = true;
   return ELLM_OK;
+}
+
+// Has a compaction given up waiting? Its tensor's rows are then not what the call's caller takes them for, so nothing goes on
+// until ellm_pool_reset_counters.
+int waits_ended(const ellm_pool* p) {
+  const uint32_t mark = p->gave_up ? __atomic_load_n(p->gave_up, __ATOMIC_RELAXED) : 0;
+  if (!mark) return ELLM_OK;
+  return set_err(ELLM_ERR_HIP, "kv_compact: a launch gave up waiting for its own flags (calls that must not overlap?); the moved rows of tensor " +
+                                   std::to_string(mark - 1) + " are undefined until they are written again, see ellm_pool_reset_counters");
 }
 
 // the append / decode calls of a pool are one sequence: what comes next runs on `stream`, behind them
@@ -507,7 +525,7 @@ int record_on(ellm_pool::Ring& r, hipStream_t stream, int64_t* seq) {
 // is therefore first put behind that one.
 int enter_compute(ellm_pool* p, hipStream_t stream, const int32_t* ids, int32_t batch, int32_t extra) {
   int rc = ensure_device(p);
-  if (rc) return rc;
+  if (rc || (rc = waits_ended(p))) return rc;
   if (p->vmm && (rc = vmm_wait_slots(p, ids, batch, extra))) return rc;
   if ((rc = follow_on(p, stream))) return rc;
   // (the table is read on this stream alone: its patch runs while the copies are still on their way. One 2 MiB chunk out, one in and a
@@ -1261,6 +1279,7 @@ int ellm_pool_destroy(ellm_pool* p) {
     for (ellm_pool::Ring* r : {&p->r_compute, &p->r_in, &p->r_out})
       for (hipEvent_t e : r->ev) (void)hipEventDestroy(e);
     (void)hipFree(p->d_table);
+    (void)hipHostFree(p->gave_up);
     if (p->ev_switch) (void)hipEventDestroy(p->ev_switch);
     for (hipEvent_t e : p->prof_ev) (void)hipEventDestroy(e);
     if (p->d_ws) (void)hipFree(p->d_ws);
@@ -1462,6 +1481,8 @@ int ellm_kv_compact(ellm_pool* p, const ellm_tensor_id* ids, int32_t batch, cons
   rc = in_groups(p, ids, batch, stream, "kv_compact launch", [&](int32_t b0, int32_t nb) {
     ellm::CompactArgs a;
     a.n_req = a.segments = 0;
+    a.looks = p->compact_looks;
+    a.gave_up = p->gave_up_dev;
     int64_t in_group = 0;
     for (int32_t i = b0; i < b0 + nb; i++) {
       if (n_keep[i] == 0) continue;
@@ -1748,7 +1769,16 @@ int ellm_pool_prepare(ellm_pool* p, void* stream) {
 
 int ellm_pool_reset_counters(ellm_pool* p, void* stream) {
   if (!p) return set_err(ELLM_ERR_INVALID, "NULL pool");
-  return p->dev_ready ? set_counters(p, 0, (hipStream_t)stream) : ELLM_OK;
+  if (!p->dev_ready) return ELLM_OK;
+  const int rc = set_counters(p, 0, (hipStream_t)stream);
+  if (!rc) __atomic_store_n(p->gave_up, 0u, __ATOMIC_RELAXED);
+  return rc;
+}
+
+int ellm_debug_set_compact_looks(ellm_pool* p, int32_t n) {
+  if (!p || n < -1) return set_err(ELLM_ERR_INVALID, "set_compact_looks: bad argument");
+  p->compact_looks = n < 0 ? ellm_pool::COMPACT_LOOKS : n;
+  return ELLM_OK;
 }
 
 int ellm_debug_set_counters(ellm_pool* p, uint32_t value, void* stream) {
@@ -1840,7 +1870,7 @@ int ellm_pool_sync(ellm_pool* p) {
   p->r_in.done = p->r_in.seq;
   HIP_TRY(hipStreamSynchronize(p->side_out), "hipStreamSynchronize(side)");
   p->r_out.done = p->r_out.seq;
-  return ELLM_OK;
+  return waits_ended(p);
 }
 
 int ellm_pool_get_geometry(ellm_pool* p, int32_t* n_chunks, int32_t* tokens_per_chunk, int32_t* n_host_slots,

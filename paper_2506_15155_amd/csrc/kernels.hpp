@@ -199,6 +199,8 @@ struct alignas(64) CopyTokenArgs {
 constexpr int COMPACT_BYTES = 64 << 10;     // of rows that a workgroup moves at a time: a segment
 struct alignas(64) CompactArgs {
   int32_t n_req, segments;         // segments of all requests, for one kv head's K (or V)
+  int32_t looks;                   // times that a wait looks at a flag before it gives up
+  uint32_t* gave_up;               // in host memory: a wait that gives up leaves its tensor's handle + 1 there
   int32_t tensor[MAX_LAUNCH_REQ];
   int32_t first[MAX_LAUNCH_REQ];
   int32_t n[MAX_LAUNCH_REQ];

@@ -214,9 +214,9 @@ __global__ __launch_bounds__(256) void copy_tokens_kernel(PoolView pv, CopyToken
 // ---------------------------------------------------------------------------------------------
 template <int D, bool FP4> constexpr int COMPACT_ROWS = COMPACT_BYTES / Rows<D, FP4>::BYTES;
 constexpr int COMPACT_THREADS = 1024;
-// A wait takes microseconds. It ends all the same (after some seconds) where something else has written over the flags, which calls in order do not.
-constexpr int32_t MOST_TURNS = 1 << 22;
-
+// A wait takes microseconds. It ends all the same (after some seconds) where something else has written over the flags, which calls in order
+// do not: the segment then stores nothing, since the rows that it would store over may not have been read yet, and says so to the host. So
+// does a workgroup whose number is none of a segment.
 template <int D, bool FP4, bool DIRECT, bool ONE_BY_ONE>
 __global__ __launch_bounds__(COMPACT_THREADS) void compact_kernel(PoolView pv, const int32_t* __restrict__ keep, uint32_t* __restrict__ marks, CompactArgs a) {
   using R = Rows<D, FP4>;
@@ -230,6 +230,9 @@ __global__ __launch_bounds__(COMPACT_THREADS) void compact_kernel(PoolView pv, c
   const int32_t* list = keep + a.key0[b];
   auto source = [&](int32_t i) __attribute__((always_inline)) { return max(first + i, min(list[i], last)); };
 
+  auto gives_up = [&]() __attribute__((always_inline)) {
+    if (threadIdx.x == 0) __hip_atomic_store(a.gave_up, (uint32_t)a.tensor[b] + 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  };
   __shared__ int32_t number;
   uint32_t* const flags = marks + gridDim.y * a.n_req * MERGE_STRIDE + (ONE_BY_ONE ? 0 : gridDim.y * a.segment0[b] + blockIdx.y * segments);
   int32_t seg = 0;
@@ -237,6 +240,7 @@ __global__ __launch_bounds__(COMPACT_THREADS) void compact_kernel(PoolView pv, c
     if (threadIdx.x == 0) number = (int32_t)atomicAdd(marks + (gridDim.y * b + blockIdx.y) * MERGE_STRIDE, 1u);
     __syncthreads();
     seg = number;
+    if ((uint32_t)seg >= (uint32_t)segments) return gives_up();
   }
   do {
     const int32_t i0 = seg * STEP;
@@ -264,10 +268,16 @@ __global__ __launch_bounds__(COMPACT_THREADS) void compact_kernel(PoolView pv, c
       if (threadIdx.x == 0) __hip_atomic_store(flags + seg, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       // the segments before this one that read as far as this one stores
       for (int32_t j = threadIdx.x; j < seg; j += COMPACT_THREADS)
-        if (source((j + 1) * STEP - 1) >= first + i0)
-          for (int32_t turn = 0; turn < MOST_TURNS && !__hip_atomic_load(flags + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); turn++)
-            __builtin_amdgcn_s_sleep(1);
+        if (source((j + 1) * STEP - 1) >= first + i0) {
+          bool seen = false;
+          for (int32_t look = 0; look < a.looks && !seen; look++) {
+            seen = __hip_atomic_load(flags + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
+            if (!seen) __builtin_amdgcn_s_sleep(1);
+          }
+          if (!seen) number = -1;            // (all have read it, two barriers ago)
+        }
       __syncthreads();
+      if (number < 0) return gives_up();
     }
 #pragma unroll
     for (int j = 0; j < N; j++) {

@@ -45,3 +45,48 @@ def test_replays_after_the_workspace_has_grown(dtype):
         c.check(c.decode(large, [c.ids[2]]), q[2:], [2])
     assert all(bool((x == 0x55).all()) for x in others)
     c.close()
+
+
+@pytest.mark.parametrize("dtype,dim", [(E.ELLM_BF16, 128), (E.ELLM_MXFP4, 64)])
+def test_a_wait_that_gives_up_is_reported_and_stores_nothing(dtype, dim):
+    """With no look at a flag every segment that has to wait leaves its rows alone; the pool says so until it is told to go on."""
+    n, first = 9000, 5
+    c = Cache([300, n, 40], 2, 2, dim, 100, dtype)
+    rows = (64 << 10) // (2 * dim if dtype == E.ELLM_BF16 else dim // 2)        # of a segment
+    assert n > 3 * rows
+    q, dq = c.queries()
+    keep = torch.arange(first + 1, n, dtype=torch.int32, device="cuda")
+    E.ellm_debug_set_compact_looks(c.pool, 0)
+    # a move of one segment waits for nothing
+    E.ellm_kv_compact(c.pool, [c.ids[0]], keep=torch.arange(0, 300, 3, dtype=torch.int32, device="cuda"), n_keep=[100])
+    c.k[0], c.v[0] = c.k[0][::3], c.v[0][::3]
+    c.decode(dq)
+    E.ellm_kv_compact(c.pool, [c.ids[1]], first=[first], keep=keep, n_keep=[len(keep)])
+    torch.cuda.synchronize()
+    lens = [E.ellm_tensor_get_table(c.pool, t)[1] for t in c.ids]
+    assert lens == [100, n - 1, 40]
+    out, rows_out = torch.empty_like(dq), torch.empty(100, 2, dim, dtype=torch.bfloat16, device="cuda")
+    refused = [lambda: E.ellm_decode_attention(c.pool, c.ids, dq, out, check=False), lambda: E.ellm_decode_attention_noalloc(c.pool, c.ids, dq, out, check=False),
+               lambda: E.ellm_kv_append(c.pool, c.ids, dq, dq, [1, 1, 1], check=False), lambda: E.ellm_kv_append_decode(c.pool, c.ids, dq, dq, dq, out, check=False),
+               lambda: E.ellm_kv_read(c.pool, [c.ids[0]], rows_out, rows_out, check=False), lambda: E.ellm_kv_copy(c.pool, [c.ids[2]], [c.ids[0]], n_tokens=[1], check=False),
+               lambda: E.ellm_kv_compact(c.pool, [c.ids[0]], keep=keep, n_keep=[1], check=False), lambda: E.ellm_pool_sync(c.pool, check=False)]
+    for call in refused:
+        assert call() == E.ERR.HIP and f"tensor {c.ids[1]} " in E.ellm_last_error()
+    assert [E.ellm_tensor_get_table(c.pool, t)[1] for t in c.ids] == lens
+    E.ellm_pool_reset_counters(c.pool)
+    E.ellm_pool_sync(c.pool)
+    # every row is the one that was to move there, or the one that was there: the first segment's all moved, the others' all not
+    for got, held in zip(read(c, [c.ids[1]]), (c.k[1], c.v[1])):
+        moved = first + rows
+        assert np.array_equal(got, np.concatenate([held[:first], held[first + 1:moved + 1], held[moved:n - 1]]))
+    # as good as new: lengths are cut, tokens appended, and the same move waits and moves
+    E.ellm_debug_set_compact_looks(c.pool, -1)
+    E.ellm_kv_compact(c.pool, [c.ids[1]])
+    c.k[1], c.v[1] = c.k[1][:0], c.v[1][:0]
+    c.append(*c.draw(n), [0, n, 0])
+    E.ellm_kv_compact(c.pool, [c.ids[1]], first=[first], keep=keep, n_keep=[len(keep)])
+    c.k[1], c.v[1] = (np.concatenate([x[1][:first], x[1][first + 1:]]) for x in (c.k, c.v))
+    same(c)
+    c.check(c.decode(dq), q)
+    assert E.ellm_debug_set_compact_looks(c.pool, -2, check=False) == E.ERR.INVALID
+    c.close()
