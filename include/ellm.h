@@ -507,7 +507,7 @@ const char* ellm_debug_decode_kernel(ellm_pool* pool, const ellm_tensor_id* ids,
  * the other split requests are added up by the attention kernel itself. Errors as of the call. For tests. */
 int ellm_debug_combined_requests(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, int32_t extra_tokens);
 /* Override the tokens per wave (rounded down to whole 64-token tiles, at least one; 0 = automatic:
- * one wave per SIMD of the GPU). For tests that compare partitions. While an override (this one or
+ * one wave per SIMD of the GPU, over 4-bit rows two where there is room). For tests that compare partitions. While an override (this one or
  * ellm_debug_set_waves) is in force, a decode call whose partition needs more partial results than
  * the workspace holds allocates a larger one, which may wait for the device; without an override that
  * cannot happen. The one before it is freed with the pool, so that graphs captured with it can be replayed. */
@@ -538,7 +538,7 @@ int ellm_debug_stream_read(const void* src, uint64_t bytes, void* sink, void* st
 int ellm_debug_kv_stream_read(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, void* sink, void* stream);
 
 /* Waves of a decode launch as a percentage (1..1600, default 100) of the library's choice, one
- * wave per SIMD of the GPU; for measurements of the work partition. Results do not depend on it
+ * wave per SIMD of the GPU (4-bit rows: up to two); for measurements of the work partition. Results do not depend on it
  * beyond rounding order. */
 int ellm_debug_set_waves(ellm_pool* pool, int32_t percent);
 /* Test hook: launches are planned as for a GPU of n compute units, as a partition of the card has them

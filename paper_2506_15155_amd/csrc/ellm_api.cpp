@@ -167,7 +167,7 @@ struct ellm_pool {
   ellm::PoolView view = {};            // what of it does not change, from pool_create on
   ellm::PairArgs pair;                 // see pair_up
   int32_t split_override = 0;
-  int32_t wave_slots = 0;              // waves of a decode launch: one per SIMD of the GPU (0 = not asked yet)
+  int32_t wave_slots = 0;              // waves of a decode launch: one or two per SIMD of the GPU (0 = not asked yet)
   int32_t compute_units = 0;           // of the GPU, known with wave_slots
   int32_t waves_percent = 100;         // waves of a launch, as a share of what the GPU holds at once
   int64_t plan_total_units = 0;        // of the launch planned last: units per kv head,
@@ -873,18 +873,22 @@ int ensure_workspace(ellm_pool* p, int64_t n_slots) {
   return ELLM_OK;
 }
 
-// Waves of a decode launch: one for every SIMD of the GPU (fewer if the kernel's resources allow
-// fewer). Two waves per SIMD, which the kernel's registers and LDS would allow, measured slower on
+// Waves of a decode launch. Over bf16 rows one for every SIMD of the GPU (fewer if the kernel's resources allow
+// fewer): two waves per SIMD, which the kernel's registers and LDS would allow, measured slower on
 // every workload: the second wave of a SIMD gets its loads served 15 to 50 % more slowly than the
-// first, and it takes bandwidth from it. Without a device (metadata-only pools, planning calls on
-// a host without GPU) a nominal MI355X figure is used: 256 compute units x 4 SIMDs.
+// first, and it takes bandwidth from it. Over 4-bit rows, whose arithmetic per byte is four times as much, two where there is room
+// (fp4_most_waves_per_cu()). Without a device (metadata-only pools, planning calls on
+// a host without GPU) a nominal MI355X is planned for: 256 compute units of 4 SIMDs.
+int32_t nominal_waves_per_cu(const ellm_pool* p) {
+  return p->geom.fp4 ? ellm::fp4_most_waves_per_cu(p->geom.head_dim, p->geom.group) : ellm::SIMDS_PER_CU;
+}
 int32_t waves_per_cu(const ellm_pool* p) {
   if (p->geom.fp4) return ellm::fp4_waves_per_cu(p->geom.head_dim, p->geom.group);
   return std::min(ellm::SIMDS_PER_CU, ellm::partial_waves_per_cu(p->geom.head_dim, p->geom.group, p->geom.tokens_per_chunk));
 }
 int32_t wave_slots(ellm_pool* p) {
   if (p->wave_slots > 0) return p->wave_slots;
-  int32_t slots = 256 * ellm::SIMDS_PER_CU;
+  int32_t slots = 256 * nominal_waves_per_cu(p);
   p->compute_units = 256;
   if (!p->metadata_only) {
     int dev = 0, cus = 0;
@@ -902,7 +906,7 @@ int32_t wave_slots(ellm_pool* p) {
 
 // The partition of one launch (at most MAX_LAUNCH_REQ requests). For each kv head the units (up to
 // UNIT_TOKENS tokens of one chunk) of all requests form one sequence, dealt out evenly to as many waves
-// as the GPU has SIMDs (all kv heads together): every wave reads the same amount to within one unit,
+// as the launch has (wave_slots(), all kv heads together): every wave reads the same amount to within one unit,
 // all are resident from the start, and a wave whose share crosses from one request into the next
 // finishes a result for each. A launch that has no STEP_UNITS units for each of them is cut at every
 // STEP_UNITS-th unit of each request instead, one wave each: a smaller share is not worth its partial
@@ -1851,7 +1855,7 @@ int ellm_debug_set_compute_units(ellm_pool* p, int32_t n) {
     return set_err(ELLM_ERR_INVALID, "set_compute_units: more than the GPU has");
   p->compute_units = n;
   // 0: asked for again by the next plan
-  p->wave_slots = n * (p->geom.fp4 && !p->metadata_only ? waves_per_cu(p) : ellm::SIMDS_PER_CU);
+  p->wave_slots = n * (p->geom.fp4 && !p->metadata_only ? waves_per_cu(p) : nominal_waves_per_cu(p));
   return ELLM_OK;
 }
 

@@ -361,7 +361,15 @@ int launch_fp4_append(const PoolView& pv, const void* k_new, const void* v_new, 
 constexpr int FP4_RUN_TOKENS = 256;
 // shares that are walked in smaller tiles (for why see kernels_fp4.hip)
 inline bool fp4_short_shares(int head_dim, const BatchArgs& a) { return head_dim == 128 && a.units_each * a.step_units < 20; }
-// waves of a compute unit that a launch which fills the GPU is cut for
+// Waves of a compute unit that a launch which fills the GPU is cut for: two workgroups of four where LDS has room for them (up to 16
+// heads of 64, 8 of 128). One wave a SIMD 343 us, two 228 (16 requests of 32768 to 131072 tokens, 8 q heads each); three and four, of
+// smaller tiles, are no faster. Over HEADS_PER_PASS heads one (a wave may leave a partial result of its own: see single_waves()).
+constexpr int FP4_TWO_WORKGROUPS = 1024;      // the most dims of all the heads that LDS is made for
+inline int fp4_most_waves_per_cu(int head_dim, int group) {
+  const int heads = group <= 4 ? 4 : group <= 8 ? 8 : HEADS_PER_PASS;
+  return group > HEADS_PER_PASS || head_dim * heads > FP4_TWO_WORKGROUPS ? SHARE_WAVES : 2 * SHARE_WAVES;
+}
+// the same on the current device, by what the kernel's resources allow
 int fp4_waves_per_cu(int head_dim, int group);
 // as launch_decode_partial and launch_decode_pair; the combine pass is the same
 int launch_fp4_decode(const PoolView& pv, const void* q, const void* k_new, const void* v_new, float* ws, void* out, float scale_log2,

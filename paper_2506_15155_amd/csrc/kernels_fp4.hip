@@ -480,7 +480,7 @@ __device__ __forceinline__ void decode_fp4_body(const PoolView& pv, const uint16
 }
 
 template <int D, int U, int HEADS, int SW, bool RUN, bool APPEND, bool DIRECT, class Args>
-__global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(D * HEADS > 1024 ? 1 : 2, D * HEADS > 1024 ? 1 : 2))) void decode_fp4_kernel(
+__global__ __launch_bounds__(64 * SW) __attribute__((amdgpu_waves_per_eu(D * HEADS > FP4_TWO_WORKGROUPS ? 1 : 2, D * HEADS > FP4_TWO_WORKGROUPS ? 1 : 2))) void decode_fp4_kernel(
     PoolView pv, const uint16_t* __restrict__ q, const char* __restrict__ k_new, const char* __restrict__ v_new,
     float* __restrict__ ws, uint16_t* __restrict__ out, float scale_log2, int32_t g_first, int32_t n_heads, Args a) {
   in_launch(pv, ws, a, [&](const PoolView& pv, float* ws, const auto& a, int32_t workgroup) __attribute__((always_inline)) {
@@ -504,9 +504,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 // wave) 19.9 us a call by 2 units, 20.8 by 4; 48, 6 q heads each 22.3, 24.6; chunks of 16 tokens 15.5, 17.0; 200 requests (28 units) 52.3,
 // 52.4; 32 of 2048 to 16384, 40 heads 268, 251; 16 of 32768 to 131072 241, 228. Heads of 64, 16 q heads, 64 of 512 to 24576 34.8, 30.5.
 constexpr int FP4_SHORT_TILE = 2, FP4_TILE = 4;
-// Two workgroups of four waves for every CU where LDS has room for them: one wave a SIMD 343 us, two 228 (16 requests of 32768 to
-// 131072 tokens, 8 q heads each); three and four, of smaller tiles, are no faster.
-constexpr int FP4_WAVES_PER_CU = 2 * SHARE_WAVES;
 
 // calls go(heads that LDS has room for) for a pass over n of them
 template <class Go>
@@ -557,7 +554,7 @@ static int launch_fp4_i(const PoolView& pv, const void* q, const void* k_new, co
 }
 
 int fp4_waves_per_cu(int head_dim, int group) {
-  if (group > HEADS_PER_PASS) return SIMDS_PER_CU;     // (a wave may leave a partial result of its own: see single_waves())
+  if (group > HEADS_PER_PASS) return fp4_most_waves_per_cu(head_dim, group);
   int n = 0;
   auto ask = [&](auto dim) {
     return for_heads(group, [&](auto h) {
@@ -567,7 +564,7 @@ int fp4_waves_per_cu(int head_dim, int group) {
   };
   const int e = head_dim == 128 ? ask(std::integral_constant<int, 128>{}) : ask(std::integral_constant<int, 64>{});
   if (e || n < 1) n = 1;
-  return std::min(n * SHARE_WAVES, FP4_WAVES_PER_CU);
+  return std::min(n * SHARE_WAVES, fp4_most_waves_per_cu(head_dim, group));
 }
 
 template <class Args>
