@@ -443,6 +443,8 @@ def ellm_kv_compact(pool, ids, first=None, keep=None, n_keep=None, flags=0, stre
     keep_i, p, n = _i32(ids)
     keep_f, pf = _i64(first, n, "first")
     keep_n, pn = _i64(n_keep, n, "n_keep")
+    if isinstance(keep, np.ndarray):
+        raise ValueError("keep: a device tensor, unlike first and n_keep")
     if hasattr(keep, "numel") and keep_n is not None:
         if keep.element_size() != 4 or not keep.is_contiguous():
             raise ValueError("keep: 32-bit positions next to each other are read")
