@@ -365,7 +365,7 @@ int ellm_kv_compact(ellm_pool* pool, const ellm_tensor_id* ids, int32_t batch, c
  *   out_h = sum_t w_t * V_t,g  for t = 0 .. len-1, no mask. scale = 0 selects 1/sqrt(head_dim).
  *   fp32 accumulation (softmax weights are rounded to bf16 before they multiply V and before they
  *   are summed, or, in some kernels, multiply V as two bf16 values; ELLM_MXFP4: weights multiply V as fp16 values, to 2^-12 of each
- *   or 2^-37 of the largest, and V counts down to 2^-36 of the largest scale that the request has in the same 32 dims), output rounded to nearest-even bf16. Split over the sequence with a partition
+ *   or 2^-37 of the largest (scores over 2^20, themselves exact to 2^-4 at best: 2^-25), and V, of any magnitude, counts down to 2^-36 of the largest scale that the request has in the same 32 dims), output rounded to nearest-even bf16. Split over the sequence with a partition
  *   that depends only on the lengths in the batch, the pool geometry and the device's wave
  *   capacity, never on physical chunk ids, so results are bitwise reproducible and invariant
  *   under remapping.

@@ -18,7 +18,7 @@
 // Products in 4 and 8 bits with scales (16x16x128) would take the codes as they are, but do not add up in 32 bits: their results
 // were 8e-5 of the sum of the products' magnitudes off.
 // 16 requests of 32768 to 131072 tokens, 8 q heads each take 228 us (6.4 TB/s, the vector unit busy for half of the time): HBM. 64 of
-// 512 to 24576, 16 q heads of 64, take 30.5 (3.5 TB/s): the vector unit, 60 % busy, between the ramp and the sums of shared requests.
+// 512 to 24576, 16 q heads of 64, take 30.7 (3.5 TB/s): the vector unit, 60 % busy, between the ramp and the sums of shared requests.
 // The K rows of the next tile are asked for when this one's scores are formed, its V rows when this one's have gone to LDS.
 #include "fp4.hpp"
 #include "fp4_walk.hpp"
@@ -37,7 +37,7 @@ __device__ __forceinline__ int32_t stage_read(int32_t row, int32_t piece, int32_
 
 // The second product is one of fp16 values, of more bits than bf16 and a smaller range, which is used to its ends. A weight is held
 // relative to the running maximum, at most 2^WEIGHT_BITS; what its rounding loses is 2^-12 of it, or, of the smallest ones, 2^-25 of
-// 1 / 2^WEIGHT_BITS: 2^-37 of the largest weight. A scale of V is held relative to the largest one of the same block that the
+// 1 / 2^WEIGHT_BITS: 2^-37 of the largest weight (2^-25 over LARGE_SCORE, below). A scale of V is held relative to the largest one of the same block that the
 // wave has met in the request, and the values are exact down to 2^-36 of it. (Weights as sums of two bf16 values, which need no such care, take twice as
 // many products and 60 more of 310 instructions a tile: 16 requests of 32768 to 131072 tokens, 8 q heads each 249 us a call.)
 constexpr int WEIGHT_BITS = 12, VALUE_BITS = 13;
