@@ -1,6 +1,7 @@
 """The list of kept positions is read by the GPU: a host array, which the counts beside it are, is refused."""
 import numpy as np
 import pytest
+import torch  # noqa: F401  (ahead of the package: both then use one HIP runtime, which the tests after this one need)
 
 import paper_2506_15155_amd as E
 

@@ -4,6 +4,7 @@ import os
 import subprocess
 
 import pytest
+import torch  # noqa: F401  (ahead of the package: both then use one HIP runtime, which the tests after this one need)
 
 import paper_2506_15155_amd as E
 
