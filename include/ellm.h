@@ -34,7 +34,7 @@
  * results, see ellm_decode_attention) and the workspace for partial
  * attention results, both allocated once by the first call that needs the device (or by
  * ellm_pool_prepare) and freed by ellm_pool_destroy; ellm_workspace_bytes tells the size of the
- * second. After that first call ellm_kv_append, ellm_decode_attention and ellm_kv_append_decode
+ * second; and a word of pinned host memory (see ellm_kv_compact). After that first call ellm_kv_append, ellm_decode_attention and ellm_kv_append_decode
  * neither allocate nor wait for the device.
  */
 #ifndef ELLM_H
